@@ -404,6 +404,74 @@ int mbu_unet_forward(const mbu_unet_desc *d, const float *image_nchw, int N, int
 int mbu_unet_forward_static(const mbu_unet_desc *d, const float *image_nchw, int N, int H, int W,
                             float *logits_nchw, void *stream);
 
+/* ---- Fully connected layers in the microscaled 4-bit format -------------------------------------------
+ *
+ * The matrix instructions that carry the masked-binary layers take 4-bit floats with a shared scale per 32 values.
+ * These operators use that format whole: activations wider than one bit, and weights either in the same format or
+ * masked-binary.
+ *
+ * Format (OCP Microscaling, MXFP4).  A row of K values is padded with zeros to Kp = 128 * ceil(K / 128).
+ *   codes   uint8 [rows][Kp / 2]: E2M1 (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two in a
+ *           byte, the lower index in the low half
+ *   scales  uint8 [rows][Kp / 32]: s stands for 2^(s - 127); 255 makes all 32 values NaN
+ * Codes beyond K must be 0 and scales beyond K must not be 255 (mbu_mx4_quantize writes 0 for both).  For K a multiple
+ * of 128 these are the plain arrays of that format.
+ *
+ * 1 <= K <= 2^23; rows, M and N are positive; every offset is computed in 64 bits.  MBU_ERR_SHAPE otherwise, and for a
+ * launch that would need 2^31 blocks.  Outputs (and the workspace) must not overlap an input: MBU_ERR_ARG.
+ * Inference only, as the rest of the library: no gradients. */
+typedef enum mbu_float_type {
+    MBU_FLOAT32 = 0,
+    MBU_FLOAT16 = 1,
+    MBU_BFLOAT16 = 2
+} mbu_float_type;
+
+/* Quantisation.  For each block: e = max(floor(log2(max |x|)) - 2, -127), s = e + 127, code = x / 2^e rounded to the
+ * nearest value of the format, ties to the even code, magnitudes above 6 to 6; a value that rounds to zero keeps its sign.
+ * A block that holds an infinity or a NaN gets s = 255 and codes 0.
+ *   x        float array of x_dtype, aligned to its type only
+ *   across   0: value k of row r is x[r * stride + k];  1: x[k * stride + r] (a weight stored input-major)
+ *   stride   in values, >= 0 (0: every row, or every k, is the same)
+ *   codes, scales  written completely, padding included */
+int mbu_mx4_quantize(const void *x, int x_dtype, int rows, int K, long long stride, int across, uint8_t *codes,
+                     uint8_t *scales, void *stream);
+
+/* The values: out[r][k] = code * 2^(s - 127), rounded once (exact in float32 and bfloat16; float16 rounds to nearest
+ * even and overflows to infinity).  out is [rows][K] of `dtype`. */
+int mbu_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype, void *stream);
+
+/* Product of two arrays of held rows, the second one holding the weights:
+ *   out[m][n] = sum_k a[m][k] * b[n][k] + bias[n]
+ * summed in float32 and rounded once to `dtype`.  The order of the sum is fixed by the shape: equal calls give equal
+ * bits.  A NaN block of a makes row m NaN, one of b column n.
+ *   bias  float32 [N] or NULL;  out [M][N] */
+int mbu_mx4_matmul(const uint8_t *a, const uint8_t *a_scales, int M, const uint8_t *b, const uint8_t *b_scales, int N,
+                   int K, const float *bias, void *out, int dtype, void *stream);
+
+/* Masked-binary weights of a fully connected layer: int8 [N][K] in {-1, 0, +1} (anything else by its sign, as in
+ * mbu_pack_weights), packed once into a blob of mbu_mx4_packed_masked_binary_bytes(N, K) bytes (two bits a weight,
+ * layout private).  A layer whose mask leaves an output nothing is fine: its sum is 0. */
+int mbu_mx4_packed_masked_binary_bytes(int N, int K, size_t *bytes);
+int mbu_mx4_pack_masked_binary(const int8_t *w, int N, int K, void *packed, void *stream);
+
+/* out[m][n] = alpha[n] * sum_k a[m][k] * w[n][k] + bias[n]: as mbu_mx4_matmul, the weights masked-binary.
+ *   packed  blob packed for (N, K') with ceil(K' / 512) = ceil(K / 512) and masked beyond K;  alpha  float32 [N] or
+ *           NULL (1).  A NaN block of a makes row m NaN, also where the weights are masked. */
+int mbu_mx4_matmul_masked_binary(const uint8_t *a, const uint8_t *a_scales, int M, const void *packed, int N, int K,
+                                 const float *alpha, const float *bias, void *out, int dtype, void *stream);
+
+/* The layer on float activations: mbu_mx4_quantize on the rows of x, then the product above, in one call.
+ *   x          [M] rows of K values of x_dtype, `stride` values apart, aligned to their type only
+ *   workspace  at least mbu_mx4_linear_workspace_bytes(M, K) bytes, not shared with a call that may run at the same
+ *              time (MBU_ERR_WORKSPACE if smaller); few rows are quantised on the way and leave it untouched */
+int mbu_mx4_linear_workspace_bytes(int M, int K, size_t *bytes);
+int mbu_mx4_linear(const void *x, int x_dtype, int M, int K, long long stride, const uint8_t *b,
+                   const uint8_t *b_scales, int N, const float *bias, void *out, int dtype, void *workspace,
+                   size_t workspace_bytes, void *stream);
+int mbu_mx4_linear_masked_binary(const void *x, int x_dtype, int M, int K, long long stride, const void *packed, int N,
+                                 const float *alpha, const float *bias, void *out, int dtype, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
 /* Thin helpers over HIP events so that a caller without HIP headers (the Python
  * binding) can time work on the stream the kernels were launched on.  Events are
  * host handles.  mbu_event_elapsed_ms synchronises on `stop`. */

@@ -24,6 +24,7 @@ MBU_ERR_NULL, MBU_ERR_SHAPE, MBU_ERR_ALIGN, MBU_ERR_WORKSPACE, MBU_ERR_HIP, MBU_
 PATH_AUTO, PATH_VALU, PATH_MFMA = 0, 1, 2
 STEM_AUTO, STEM_VALU, STEM_MFMA, STEM_MFMA_GATHER = 0, 1, 2, 3
 STATIC_WORKSPACE_BYTES = 32 << 20
+FLOAT32, FLOAT16, BFLOAT16 = 0, 1, 2
 BLOB_BIT_PLANES, BLOB_SUMMED_TAPS, BLOB_MATRIX, BLOB_ALL = 1, 2, 4, 7
 
 EXPORTS = [
@@ -38,6 +39,9 @@ EXPORTS = [
     "mbu_maxpool2x2_bits", "mbu_upsample2x_bits", "mbu_concat_bits", "mbu_unet_num_steps",
     "mbu_unet_step_info", "mbu_unet_step_launches", "mbu_unet_workspace_bytes", "mbu_unet_forward",
     "mbu_unet_forward_static",
+    "mbu_mx4_quantize", "mbu_mx4_dequantize", "mbu_mx4_matmul", "mbu_mx4_packed_masked_binary_bytes",
+    "mbu_mx4_pack_masked_binary", "mbu_mx4_matmul_masked_binary", "mbu_mx4_linear_workspace_bytes", "mbu_mx4_linear",
+    "mbu_mx4_linear_masked_binary",
     "mbu_event_create", "mbu_event_destroy", "mbu_event_record", "mbu_event_elapsed_ms",
 ]
 
@@ -113,6 +117,16 @@ def lib() -> ctypes.CDLL:
         L.mbu_unet_forward.argtypes = [ctypes.POINTER(UNetDesc), vp, ci, ci, ci, vp, vp,
                                        ctypes.c_size_t, vp]
         L.mbu_unet_forward_static.argtypes = [ctypes.POINTER(UNetDesc), vp, ci, ci, ci, vp, vp]
+        ll, sz = ctypes.c_longlong, ctypes.c_size_t
+        L.mbu_mx4_quantize.argtypes = [vp, ci, ci, ci, ll, ci, vp, vp, vp]
+        L.mbu_mx4_dequantize.argtypes = [vp, vp, ci, ci, vp, ci, vp]
+        L.mbu_mx4_matmul.argtypes = [vp, vp, ci, vp, vp, ci, ci, vp, vp, ci, vp]
+        L.mbu_mx4_packed_masked_binary_bytes.argtypes = [ci, ci, ctypes.POINTER(sz)]
+        L.mbu_mx4_pack_masked_binary.argtypes = [vp, ci, ci, vp, vp]
+        L.mbu_mx4_matmul_masked_binary.argtypes = [vp, vp, ci, vp, ci, ci, vp, vp, vp, ci, vp]
+        L.mbu_mx4_linear_workspace_bytes.argtypes = [ci, ci, ctypes.POINTER(sz)]
+        L.mbu_mx4_linear.argtypes = [vp, ci, ci, ci, ll, vp, vp, ci, vp, vp, ci, vp, sz, vp]
+        L.mbu_mx4_linear_masked_binary.argtypes = [vp, ci, ci, ci, ll, vp, ci, vp, vp, vp, ci, vp, sz, vp]
         L.mbu_event_create.argtypes = [ctypes.POINTER(vp)]
         L.mbu_event_destroy.argtypes = [vp]
         L.mbu_event_record.argtypes = [vp, vp]
@@ -466,6 +480,178 @@ def concat_bits(a: torch.Tensor, ca: int, b: torch.Tensor, cb: int) -> torch.Ten
     out = torch.empty((N, H, W, Caw + b.shape[3]), dtype=torch.int32, device=a.device)
     check(lib().mbu_concat_bits(_dev(a, (torch.int32,)), ca, _dev(b, (torch.int32,)), cb, N, H, W,
                                 out.data_ptr(), _stream()))
+    return out
+
+
+# Microscaled 4-bit format: codes uint8 [rows, Kp / 2], scales uint8 [rows, Kp / 32], Kp = K rounded up to 128.
+_FLOATS = {torch.float32: FLOAT32, torch.float16: FLOAT16, torch.bfloat16: BFLOAT16}
+
+
+def _here(what: str, t: torch.Tensor, dtypes, dim: int) -> torch.Tensor:
+    """The tensor, if it is what a call on the current device's stream can take."""
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: expected dtype in {tuple(dtypes)}, got {t.dtype}")
+    if t.dim() != dim:
+        raise ValueError(f"{what}: expected {dim} dimensions, got {t.dim()}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return t
+
+
+def _held(what: str, codes: torch.Tensor, scales: torch.Tensor) -> Tuple[int, int]:
+    """(rows, Kp) of a pair of codes and scales."""
+    _here(what, codes, (torch.uint8,), 2)
+    _here(what + " scales", scales, (torch.uint8,), 2)
+    rows, kp = codes.shape[0], 2 * codes.shape[1]
+    if kp % 128 or tuple(scales.shape) != (rows, kp // 32):
+        raise ValueError(f"{what}: codes [rows, Kp / 2] and scales [rows, Kp / 32] with Kp a multiple of 128, got "
+                         f"{tuple(codes.shape)} and {tuple(scales.shape)}")
+    if not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    return rows, kp
+
+
+def _per_output(what: str, t: Optional[torch.Tensor], n: int) -> Optional[int]:
+    if t is None:
+        return None
+    _here(what, t, (torch.float32,), 1)
+    if t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {n} contiguous values")
+    return t.data_ptr()
+
+
+def _float_code(dtype: torch.dtype) -> int:
+    if dtype not in _FLOATS:
+        raise ValueError(f"expected dtype in {tuple(_FLOATS)}, got {dtype}")
+    return _FLOATS[dtype]
+
+
+def mx4_quantize(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """mbu_mx4_quantize: x [rows, K] float32, float16 or bfloat16 -> (codes, scales).  One of x's strides has to be 1
+    (a transposed view of a weight stored input-major is read in place)."""
+    _here("x", x, _FLOATS, 2)
+    rows, k = x.shape
+    s0, s1 = x.stride()
+    if k > 1 and s1 != 1 and rows > 1 and s0 != 1:
+        raise ValueError("expected one of the strides of x to be 1")
+    across = k > 1 and s1 != 1
+    kp = (k + 127) // 128 * 128
+    codes = torch.empty((rows, kp // 2), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((rows, kp // 32), dtype=torch.uint8, device=x.device)
+    check(lib().mbu_mx4_quantize(x.data_ptr(), _FLOATS[x.dtype], rows, k, s1 if across else s0, 1 if across else 0,
+                                 codes.data_ptr(), scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: torch.dtype = torch.float32
+                   ) -> torch.Tensor:
+    """mbu_mx4_dequantize: the values [rows, k] of held rows."""
+    rows, kp = _held("codes", codes, scales)
+    if not kp - 128 < k <= kp:
+        raise ValueError(f"rows of {kp} codes do not hold {k} values")
+    out = torch.empty((rows, k), dtype=dtype, device=codes.device)
+    check(lib().mbu_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, out.data_ptr(), _float_code(dtype),
+                                   _stream()))
+    return out
+
+
+def mx4_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+               bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """mbu_mx4_matmul: held rows a [M] and b [N] of the same K -> a b^T + bias, [M, N] of `dtype`."""
+    m, kp = _held("a", a, a_scales)
+    n, kb = _held("b", b, b_scales)
+    if kb != kp:
+        raise ValueError(f"a has rows of {kp} values, b of {kb}")
+    code = _float_code(dtype)
+    pb = _per_output("bias", bias, n)
+    out = torch.empty((m, n), dtype=dtype, device=a.device)
+    check(lib().mbu_mx4_matmul(a.data_ptr(), a_scales.data_ptr(), m, b.data_ptr(), b_scales.data_ptr(), n, kp, pb,
+                               out.data_ptr(), code, _stream()))
+    return out
+
+
+def _mx4_blob_bytes(n: int, k: int) -> int:
+    size = ctypes.c_size_t(0)
+    check(lib().mbu_mx4_packed_masked_binary_bytes(n, k, ctypes.byref(size)))
+    return size.value
+
+
+def mx4_pack_masked_binary(w: torch.Tensor) -> torch.Tensor:
+    """mbu_mx4_pack_masked_binary: device int8 [N, K] in {-1, 0, +1} -> opaque blob (uint8 tensor)."""
+    _here("w", w, (torch.int8,), 2)
+    n, k = w.shape
+    blob = torch.empty(_mx4_blob_bytes(n, k), dtype=torch.uint8, device=w.device)
+    check(lib().mbu_mx4_pack_masked_binary(_dev(w, (torch.int8,)), n, k, blob.data_ptr(), _stream()))
+    return blob
+
+
+def _blob(packed: torch.Tensor, n: int, k: int) -> int:
+    _here("packed", packed, (torch.uint8,), 1)
+    if packed.numel() != _mx4_blob_bytes(n, k):
+        raise ValueError(f"packed holds {packed.numel()} bytes, a layer of {n} x {k} has {_mx4_blob_bytes(n, k)}")
+    return _dev(packed, (torch.uint8,))
+
+
+def mx4_matmul_masked_binary(a: torch.Tensor, a_scales: torch.Tensor, packed: torch.Tensor, n: int,
+                             alpha: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                             dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """mbu_mx4_matmul_masked_binary: held rows a [M], blob of n outputs -> alpha * (a w^T) + bias, [M, n] of `dtype`."""
+    m, kp = _held("a", a, a_scales)
+    code = _float_code(dtype)
+    pw = _blob(packed, n, kp)
+    pa, pb = _per_output("alpha", alpha, n), _per_output("bias", bias, n)
+    out = torch.empty((m, n), dtype=dtype, device=a.device)
+    check(lib().mbu_mx4_matmul_masked_binary(a.data_ptr(), a_scales.data_ptr(), m, pw, n, kp, pa, pb, out.data_ptr(),
+                                             code, _stream()))
+    return out
+
+
+def _linear_input(x: torch.Tensor) -> Tuple[int, int, int]:
+    """(M, K, distance of the rows) of float activations."""
+    _here("x", x, _FLOATS, 2)
+    m, k = x.shape
+    if k > 1 and x.stride(1) != 1:
+        raise ValueError("expected rows of consecutive values")
+    return m, k, x.stride(0)
+
+
+def _linear_workspace(m: int, k: int, device) -> torch.Tensor:
+    size = ctypes.c_size_t(0)
+    check(lib().mbu_mx4_linear_workspace_bytes(m, k, ctypes.byref(size)))
+    return torch.empty(size.value, dtype=torch.uint8, device=device)
+
+
+def mx4_linear(x: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
+               dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """mbu_mx4_linear: x [M, K] floats, held weights [N] -> quantised x times b^T + bias, [M, N] of `dtype` (x's)."""
+    m, k, stride = _linear_input(x)
+    n, kp = _held("b", b, b_scales)
+    if not kp - 128 < k <= kp:
+        raise ValueError(f"x has rows of {k} values, b of {kp}")
+    dtype = x.dtype if dtype is None else dtype
+    code = _float_code(dtype)
+    pb = _per_output("bias", bias, n)
+    ws = _linear_workspace(m, k, x.device)
+    out = torch.empty((m, n), dtype=dtype, device=x.device)
+    check(lib().mbu_mx4_linear(x.data_ptr(), _FLOATS[x.dtype], m, k, stride, b.data_ptr(), b_scales.data_ptr(), n, pb,
+                               out.data_ptr(), code, ws.data_ptr(), ws.numel(), _stream()))
+    return out
+
+
+def mx4_linear_masked_binary(x: torch.Tensor, packed: torch.Tensor, n: int, alpha: Optional[torch.Tensor] = None,
+                             bias: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """mbu_mx4_linear_masked_binary: the same with masked-binary weights (blob of n outputs) and their factors."""
+    m, k, stride = _linear_input(x)
+    dtype = x.dtype if dtype is None else dtype
+    code = _float_code(dtype)
+    pw = _blob(packed, n, k)
+    pa, pb = _per_output("alpha", alpha, n), _per_output("bias", bias, n)
+    ws = _linear_workspace(m, k, x.device)
+    out = torch.empty((m, n), dtype=dtype, device=x.device)
+    check(lib().mbu_mx4_linear_masked_binary(x.data_ptr(), _FLOATS[x.dtype], m, k, stride, pw, n, pa, pb,
+                                             out.data_ptr(), code, ws.data_ptr(), ws.numel(), _stream()))
     return out
 
 

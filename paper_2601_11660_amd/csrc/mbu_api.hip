@@ -83,12 +83,6 @@ static int check_dims4(const char *fn, int N, int H, int W, int C)
     return MBU_OK;
 }
 
-#define MBU_REQ_PTR(fn, p)                                                        \
-    do {                                                                          \
-        if ((p) == nullptr) return mbu::fail(MBU_ERR_NULL, "%s: %s is NULL", fn, #p); \
-        if (!mbu::aligned16(p)) return mbu::fail(MBU_ERR_ALIGN, "%s: %s is not 16-byte aligned", fn, #p); \
-    } while (0)
-
 // layout of a network layer's blob: `sections` 0 means a blob from mbu_pack_weights (everything)
 static BlobLayout layer_layout(const mbu_conv_layer &L)
 {

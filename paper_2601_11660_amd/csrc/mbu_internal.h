@@ -48,6 +48,13 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline size_t round_up(size_t v, size_t m) { return (v + m - 1) / m * m; }
 
+// a required device pointer of an entry point
+#define MBU_REQ_PTR(fn, p)                                                        \
+    do {                                                                          \
+        if ((p) == nullptr) return mbu::fail(MBU_ERR_NULL, "%s: %s is NULL", fn, #p); \
+        if (!mbu::aligned16(p)) return mbu::fail(MBU_ERR_ALIGN, "%s: %s is not 16-byte aligned", fn, #p); \
+    } while (0)
+
 // ---- layout of the packed-weight blob (all offsets in bytes from the blob start) ----
 // Section V (vector-ALU path, optional: MBU_BLOB_BIT_PLANES): two bit planes, each uint32
 // [9][cin_words][cout_pad64] (tap-major, output channel fastest so 64 lanes read 64
@@ -161,5 +168,34 @@ int launch_stem_mfma(const float *img, int N, int Ci, int H, int W, const float 
                      uint32_t *out_bits, float *out_pre, hipStream_t s);
 int launch_classifier(const uint32_t *act, int N, int H, int W, int C, const float *w,
                       const float *b, int K, float *out, hipStream_t s);
+
+// ---- microscaled 4-bit format ----
+inline int mx4_padded(int K) { return (K + 127) / 128 * 128; }
+// Blob of masked-binary weights of a fully connected layer: uint4 [tiles][steps][2][64 lanes], tile = 16 outputs,
+// step = 512 inputs; lane l of half h holds inputs 128 (l / 16) + 64 h + 0..63 of the step of output l % 16, two bits
+// each (mx4_common.h: expand_masked); what lies beyond N and K is masked.
+struct Mx4MaskedLayout {
+    int tiles, steps;
+    size_t bytes;
+};
+inline Mx4MaskedLayout mx4_masked_layout(int N, int K)
+{
+    const int tiles = ceil_div(N, 16), steps = ceil_div(mx4_padded(K), 512);
+    return {tiles, steps, (size_t)tiles * steps * 2048};
+}
+// can rows of floats be read 16 bytes at a time?
+inline bool mx4_rows_aligned(const void *x, size_t size, int rows, int K, long long stride)
+{
+    return aligned16(x) && (K * size) % 16 == 0 && (rows == 1 || (stride * (long long)size) % 16 == 0);
+}
+int launch_mx4_quantize(const void *x, int dtype, int rows, int K, long long stride, bool across, uint8_t *codes,
+                        uint8_t *scales, hipStream_t s);
+int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype,
+                          hipStream_t s);
+int launch_mx4_pack_masked(const int8_t *w, int N, int K, void *packed, hipStream_t s);
+// masked: w is a blob of masked-binary weights, else codes with scales ws; alpha, bias: float32 [N] or NULL
+int launch_mx4_matmul(const char *fn, const uint8_t *a, const uint8_t *as, int M, bool masked, const void *w,
+                      const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
+                      hipStream_t s);
 
 }  // namespace mbu

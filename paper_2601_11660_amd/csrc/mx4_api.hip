@@ -1,0 +1,227 @@
+// C-ABI entry points of the microscaled 4-bit operators: argument checks and dispatch.
+#include "mx4_common.h"
+
+namespace mbu {
+
+constexpr int MX4_MOST_K = 1 << 23;      // offsets inside a tile of rows stay below 2 GiB
+
+static size_t float_size(int dtype) { return dtype == MBU_FLOAT32 ? 4 : 2; }
+
+static int check_dtype(const char *fn, const char *what, int dtype)
+{
+    if (dtype != MBU_FLOAT32 && dtype != MBU_FLOAT16 && dtype != MBU_BFLOAT16)
+        return fail(MBU_ERR_ARG, "%s: unknown %s %d", fn, what, dtype);
+    return MBU_OK;
+}
+
+static int check_rows(const char *fn, const char *what, int rows, int K)
+{
+    if (rows <= 0 || K <= 0) return fail(MBU_ERR_SHAPE, "%s: dimensions must be positive (%s=%d K=%d)", fn, what, rows, K);
+    if (K > MX4_MOST_K) return fail(MBU_ERR_SHAPE, "%s: K must be at most %d, got %d", fn, MX4_MOST_K, K);
+    return MBU_OK;
+}
+
+static size_t code_bytes(int rows, int K) { return (size_t)rows * (mx4_padded(K) / 2); }
+static size_t scale_bytes(int rows, int K) { return (size_t)rows * (mx4_padded(K) / 32); }
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+// float rows: only the alignment of their type is needed
+static int check_float_rows(const char *fn, const void *x, int dtype, int rows, int K, long long stride)
+{
+    if (!x) return fail(MBU_ERR_NULL, "%s: x is NULL", fn);
+    if ((uintptr_t)x % float_size(dtype)) return fail(MBU_ERR_ALIGN, "%s: x is not aligned to its type", fn);
+    if (stride < 0 || stride > (1ll << 40)) return fail(MBU_ERR_SHAPE, "%s: stride %lld out of range", fn, stride);
+    (void)rows;
+    (void)K;
+    return MBU_OK;
+}
+// bytes from the first to behind the last value
+static size_t float_extent(int dtype, int rows, int K, long long stride)
+{
+    return ((size_t)(rows - 1) * (size_t)stride + (size_t)K) * float_size(dtype);
+}
+
+struct Mx4Product {
+    bool masked;
+    const void *w;
+    const uint8_t *ws;
+    int N, K;
+    const float *alpha, *bias;
+    void *out;
+    int dtype;
+};
+
+// what the two forms of the product and the two of the linear layer have in common
+static int check_product(const char *fn, int M, const Mx4Product &p)
+{
+    int rc = check_rows(fn, "M", M, p.K);
+    if (!rc) rc = check_rows(fn, "N", p.N, p.K);
+    if (!rc) rc = check_dtype(fn, "dtype", p.dtype);
+    if (rc) return rc;
+    const void *const weights = p.w, *const out = p.out;
+    MBU_REQ_PTR(fn, weights);
+    MBU_REQ_PTR(fn, out);
+    if (!p.masked) {
+        const uint8_t *const weight_scales = p.ws;
+        MBU_REQ_PTR(fn, weight_scales);
+    }
+    if (!aligned16(p.alpha)) return fail(MBU_ERR_ALIGN, "%s: alpha is not 16-byte aligned", fn);
+    if (!aligned16(p.bias)) return fail(MBU_ERR_ALIGN, "%s: bias is not 16-byte aligned", fn);
+    const size_t n = (size_t)M * p.N * float_size(p.dtype);
+    const size_t nw = p.masked ? mx4_masked_layout(p.N, p.K).bytes : code_bytes(p.N, p.K);
+    if (overlap(out, n, weights, nw) || overlap(out, n, p.ws, scale_bytes(p.N, p.K)) ||
+        overlap(out, n, p.alpha, (size_t)p.N * 4) || overlap(out, n, p.bias, (size_t)p.N * 4))
+        return fail(MBU_ERR_ARG, "%s: the output must not alias an input", fn);
+    return MBU_OK;
+}
+
+static int matmul(const char *fn, const uint8_t *a, const uint8_t *a_scales, int M, const Mx4Product &p, void *stream)
+{
+    begin_call();
+    MBU_REQ_PTR(fn, a);
+    MBU_REQ_PTR(fn, a_scales);
+    const int rc = check_product(fn, M, p);
+    if (rc) return rc;
+    const size_t n = (size_t)M * p.N * float_size(p.dtype);
+    if (overlap(p.out, n, a, code_bytes(M, p.K)) || overlap(p.out, n, a_scales, scale_bytes(M, p.K)))
+        return fail(MBU_ERR_ARG, "%s: the output must not alias an input", fn);
+    return launch_mx4_matmul(fn, a, a_scales, M, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out, p.dtype,
+                             (hipStream_t)stream);
+}
+
+static size_t linear_workspace(int M, int K) { return round_up(code_bytes(M, K), 256) + round_up(scale_bytes(M, K), 256); }
+
+static int linear(const char *fn, const void *x, int x_dtype, int M, long long stride, const Mx4Product &p,
+                  void *workspace, size_t workspace_bytes, void *stream)
+{
+    begin_call();
+    int rc = check_dtype(fn, "x_dtype", x_dtype);
+    if (!rc) rc = check_product(fn, M, p);
+    if (!rc) rc = check_float_rows(fn, x, x_dtype, M, p.K, stride);
+    if (rc) return rc;
+    MBU_REQ_PTR(fn, workspace);
+    const size_t need = linear_workspace(M, p.K), n = (size_t)M * p.N * float_size(p.dtype);
+    if (workspace_bytes < need)
+        return fail(MBU_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
+    const size_t nx = float_extent(x_dtype, M, p.K, stride);
+    const size_t nw = p.masked ? mx4_masked_layout(p.N, p.K).bytes : code_bytes(p.N, p.K);
+    if (overlap(p.out, n, x, nx) || overlap(workspace, need, x, nx) || overlap(workspace, need, p.out, n) ||
+        overlap(workspace, need, p.w, nw) || overlap(workspace, need, p.ws, scale_bytes(p.N, p.K)) ||
+        overlap(workspace, need, p.alpha, (size_t)p.N * 4) || overlap(workspace, need, p.bias, (size_t)p.N * 4))
+        return fail(MBU_ERR_ARG, "%s: output and workspace must not alias an input or each other", fn);
+    uint8_t *const codes = (uint8_t *)workspace, *const scales = codes + round_up(code_bytes(M, p.K), 256);
+    rc = launch_mx4_quantize(x, x_dtype, M, p.K, stride, false, codes, scales, (hipStream_t)stream);
+    if (rc) return rc;
+    return launch_mx4_matmul(fn, codes, scales, M, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out, p.dtype,
+                             (hipStream_t)stream);
+}
+
+}  // namespace mbu
+
+using namespace mbu;
+
+extern "C" {
+
+int mbu_mx4_quantize(const void *x, int x_dtype, int rows, int K, long long stride, int across, uint8_t *codes,
+                     uint8_t *scales, void *stream)
+{
+    const char *fn = "mbu_mx4_quantize";
+    begin_call();
+    int rc = check_rows(fn, "rows", rows, K);
+    if (!rc) rc = check_dtype(fn, "x_dtype", x_dtype);
+    if (!rc) rc = check_float_rows(fn, x, x_dtype, rows, K, stride);
+    if (rc) return rc;
+    if (across != 0 && across != 1) return fail(MBU_ERR_ARG, "%s: across must be 0 or 1, got %d", fn, across);
+    MBU_REQ_PTR(fn, codes);
+    MBU_REQ_PTR(fn, scales);
+    const size_t nx = across ? float_extent(x_dtype, K, rows, stride) : float_extent(x_dtype, rows, K, stride);
+    if (overlap(codes, code_bytes(rows, K), x, nx) || overlap(scales, scale_bytes(rows, K), x, nx) ||
+        overlap(codes, code_bytes(rows, K), scales, scale_bytes(rows, K)))
+        return fail(MBU_ERR_ARG, "%s: outputs must not alias the input or each other", fn);
+    return launch_mx4_quantize(x, x_dtype, rows, K, stride, across != 0, codes, scales, (hipStream_t)stream);
+}
+
+int mbu_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype, void *stream)
+{
+    const char *fn = "mbu_mx4_dequantize";
+    begin_call();
+    MBU_REQ_PTR(fn, codes);
+    MBU_REQ_PTR(fn, scales);
+    MBU_REQ_PTR(fn, out);
+    int rc = check_rows(fn, "rows", rows, K);
+    if (!rc) rc = check_dtype(fn, "dtype", dtype);
+    if (rc) return rc;
+    const size_t n = (size_t)rows * K * float_size(dtype);
+    if (overlap(out, n, codes, code_bytes(rows, K)) || overlap(out, n, scales, scale_bytes(rows, K)))
+        return fail(MBU_ERR_ARG, "%s: the output must not alias an input", fn);
+    return launch_mx4_dequantize(codes, scales, rows, K, out, dtype, (hipStream_t)stream);
+}
+
+int mbu_mx4_packed_masked_binary_bytes(int N, int K, size_t *bytes)
+{
+    const char *fn = "mbu_mx4_packed_masked_binary_bytes";
+    if (!bytes) return fail(MBU_ERR_NULL, "%s: bytes is NULL", fn);
+    const int rc = check_rows(fn, "N", N, K);
+    if (rc) return rc;
+    *bytes = mx4_masked_layout(N, K).bytes;
+    return MBU_OK;
+}
+
+int mbu_mx4_pack_masked_binary(const int8_t *w, int N, int K, void *packed, void *stream)
+{
+    const char *fn = "mbu_mx4_pack_masked_binary";
+    begin_call();
+    MBU_REQ_PTR(fn, w);
+    MBU_REQ_PTR(fn, packed);
+    const int rc = check_rows(fn, "N", N, K);
+    if (rc) return rc;
+    if (overlap(packed, mx4_masked_layout(N, K).bytes, w, (size_t)N * K))
+        return fail(MBU_ERR_ARG, "%s: the output must not alias the input", fn);
+    return launch_mx4_pack_masked(w, N, K, packed, (hipStream_t)stream);
+}
+
+int mbu_mx4_matmul(const uint8_t *a, const uint8_t *a_scales, int M, const uint8_t *b, const uint8_t *b_scales, int N,
+                   int K, const float *bias, void *out, int dtype, void *stream)
+{
+    return matmul("mbu_mx4_matmul", a, a_scales, M, Mx4Product{false, b, b_scales, N, K, nullptr, bias, out, dtype}, stream);
+}
+
+int mbu_mx4_matmul_masked_binary(const uint8_t *a, const uint8_t *a_scales, int M, const void *packed, int N, int K,
+                                 const float *alpha, const float *bias, void *out, int dtype, void *stream)
+{
+    return matmul("mbu_mx4_matmul_masked_binary", a, a_scales, M,
+                  Mx4Product{true, packed, nullptr, N, K, alpha, bias, out, dtype}, stream);
+}
+
+int mbu_mx4_linear_workspace_bytes(int M, int K, size_t *bytes)
+{
+    const char *fn = "mbu_mx4_linear_workspace_bytes";
+    if (!bytes) return fail(MBU_ERR_NULL, "%s: bytes is NULL", fn);
+    const int rc = check_rows(fn, "M", M, K);
+    if (rc) return rc;
+    *bytes = linear_workspace(M, K);
+    return MBU_OK;
+}
+
+int mbu_mx4_linear(const void *x, int x_dtype, int M, int K, long long stride, const uint8_t *b,
+                   const uint8_t *b_scales, int N, const float *bias, void *out, int dtype, void *workspace,
+                   size_t workspace_bytes, void *stream)
+{
+    return linear("mbu_mx4_linear", x, x_dtype, M, stride, Mx4Product{false, b, b_scales, N, K, nullptr, bias, out, dtype},
+                  workspace, workspace_bytes, stream);
+}
+
+int mbu_mx4_linear_masked_binary(const void *x, int x_dtype, int M, int K, long long stride, const void *packed, int N,
+                                 const float *alpha, const float *bias, void *out, int dtype, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    return linear("mbu_mx4_linear_masked_binary", x, x_dtype, M, stride,
+                  Mx4Product{true, packed, nullptr, N, K, alpha, bias, out, dtype}, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -172,8 +172,8 @@ int launch_classifier(const uint32_t *act, int N, int H, int W, int C, const flo
 // ---- microscaled 4-bit format ----
 inline int mx4_padded(int K) { return (K + 127) / 128 * 128; }
 // Blob of masked-binary weights of a fully connected layer: uint4 [tiles][steps][2][64 lanes], tile = 16 outputs,
-// step = 512 inputs; lane l of half h holds inputs 128 (l / 16) + 64 h + 0..63 of the step of output l % 16, two bits
-// each (mx4_common.h: expand_masked); what lies beyond N and K is masked.
+// step = 512 inputs; lane l of half h holds inputs 256 h + 32 (l / 16) + 0..31 and the same + 128 of the step of output
+// l % 16, two bits each (mx4_common.h: expand_masked); what lies beyond N and K is masked.
 struct Mx4MaskedLayout {
     int tiles, steps;
     size_t bytes;

@@ -126,6 +126,21 @@ template <> struct Mx4In<_Float16> {
 // the conversions read the exponent field of the scale alone: 2^-127, whose float32 form is a subnormal, is 0 here
 __device__ __forceinline__ float mx4_scale_float(uint32_t s) { return __uint_as_float(s << 23); }
 
+// The 16 scale bytes of a row's 512 inputs -> the four that lane group g multiplies with, byte j for instruction j:
+// bytes g, 4 + g, 8 + g, 12 + g
+__device__ __forceinline__ uint32_t mx4_scales_of(v4i s, int g)
+{
+    const uint32_t pick = 0x0400u + 0x0101u * (uint32_t)g;          // byte g of the second word, byte g of the first
+    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)s.y, (uint32_t)s.x, pick);
+    const uint32_t hi = __builtin_amdgcn_perm((uint32_t)s.w, (uint32_t)s.z, pick);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+// ... of a row that has `left` scale bytes left (a multiple of four; what follows belongs to another row)
+__device__ __forceinline__ v4i mx4_row_end(v4i s, int left)
+{
+    return (v4i){left > 0 ? s.x : 0, left > 4 ? s.y : 0, left > 8 ? s.z : 0, left > 12 ? s.w : 0};
+}
+
 // Masked-binary weights: two bits a weight, 16 in a word.  Nibble q holds weight q in bits 3 (sign) and 1 (kept) and
 // weight q + 8 in bits 2 and 0, so that a mask makes eight codes of either half: -1 is 0b1010, +1 is 0b0010.
 __device__ __forceinline__ v4i expand_masked(uint32_t w0, uint32_t w1)

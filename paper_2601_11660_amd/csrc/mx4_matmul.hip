@@ -2,26 +2,13 @@
 //
 //   y[m][n] = alpha[n] * sum_k a[m][k] w[n][k] + bias[n]
 //
-// A matrix instruction takes 16 rows by 128 inputs of either operand, a lane 32 inputs (one scale block) of one row.
-// Which blocks of a row the four lane groups g = lane / 16 take is free, so 512 inputs form a step in which group g owns
-// inputs 128 g .. 128 g + 127: 64 consecutive bytes of codes, four instructions, and exactly one aligned word of scales,
-// whose byte j belongs to instruction j.  Weights are the first operand, so a lane gets four consecutive outputs.
-#include "mx4_common.h"
+// A matrix instruction takes 16 rows by 128 inputs of either operand; lane l holds inputs 32 (l / 16) .. + 31 (one scale
+// block, 16 bytes) of row l % 16, so that a wave reads 64 consecutive bytes of every row.  The sum runs in steps of 512
+// inputs: four instructions and 16 scale bytes a row, of which a lane keeps four in one word, byte j for instruction j.
+// Weights are the first operand, so a lane gets four consecutive outputs.
+#include "mx4_product.h"
 
 namespace mbu {
-
-struct Mx4Args {
-    const void *x;              // held: codes [M][kp/2]; float: rows `ldx` apart
-    const uint8_t *xs;          // held: scales [M][kp/32]
-    const void *w;              // held: codes [N][kp/2]; masked: blob
-    const uint8_t *ws;          // held: scales [N][kp/32]
-    const float *alpha, *bias;  // [N] or NULL
-    void *out;
-    long long ldx;
-    int M, N, K, kp, steps, tiles_n;
-};
-
-enum Mx4Weights { W_HELD, W_MASKED };
 
 struct Mx4Frag {
     v4i c[4];
@@ -32,17 +19,19 @@ struct Mx4Frag {
 __device__ __forceinline__ void load_held(Mx4Frag &f, const uint8_t *codes, const uint8_t *scales, long long row,
                                           int kp, int step, int g)
 {
-    const int byte = step * 256 + g * 64;
-    const bool ok = byte < (kp >> 1);
-    const int at = ok ? byte : 0;
-    const uint4 *p = reinterpret_cast<const uint4 *>(codes + row * (kp >> 1) + at);
+    const uint4 *p = reinterpret_cast<const uint4 *>(codes + row * (kp >> 1) + step * 256 + g * 16);
+    const uint32_t *q = reinterpret_cast<const uint32_t *>(scales + row * (kp >> 5) + step * 16);
+    v4i s = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint4 v = p[j];
-        f.c[j] = ok ? (v4i){(int)v.x, (int)v.y, (int)v.z, (int)v.w} : (v4i){0, 0, 0, 0};
+        uint4 v = {0, 0, 0, 0};
+        if (step * 512 + j * 128 < kp) {
+            v = p[4 * j];
+            s[j] = (int)q[j];
+        }
+        f.c[j] = (v4i){(int)v.x, (int)v.y, (int)v.z, (int)v.w};
     }
-    const uint32_t s = *reinterpret_cast<const uint32_t *>(scales + row * (kp >> 5) + (at >> 4));
-    f.s = ok ? s : 0u;
+    f.s = mx4_scales_of(s, g);
 }
 
 // the same from a blob of masked-binary weights (every scale 2^0)
@@ -65,7 +54,7 @@ __device__ __forceinline__ void load_float(Mx4Frag &f, const T *row, int K, int 
     f.s = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int k0 = step * 512 + g * 128 + j * 32;
+        const int k0 = step * 512 + j * 128 + g * 32;
         Mx4In<T> in[4];
         uint32_t top = 0;
 #pragma unroll
@@ -184,6 +173,7 @@ int launch_mx4_matmul(const char *fn, const uint8_t *a, const uint8_t *as, int M
 {
     const int kp = mx4_padded(K);
     const Mx4Args p = {a, as, w, ws, alpha, bias, out, 0, M, N, K, kp, ceil_div(kp, 512), 0};
+    if (M > 64) return launch_mx4_tile(fn, p, masked, dtype, s);
     if (dtype == MBU_FLOAT32) return choose_weights<uint8_t, float>(fn, p, masked, s);
     if (dtype == MBU_FLOAT16) return choose_weights<uint8_t, _Float16>(fn, p, masked, s);
     return choose_weights<uint8_t, __bf16>(fn, p, masked, s);

@@ -136,13 +136,14 @@ __global__ __launch_bounds__(256) void mx4_pack_masked_kernel(const int8_t *__re
     const long long t = u >> 7;                     // 16 outputs x 512 inputs
     const int step = (int)(t % steps);
     const long long n = t / steps * 16 + (lane & 15);
-    const long long k0 = (long long)step * 512 + (lane >> 4) * 128 + half * 64;
+    const long long k0 = (long long)step * 512 + half * 256 + (lane >> 4) * 32;
     uint32_t word[4] = {0, 0, 0, 0};
     if (n < N) {
         const int8_t *src = w + n * K;
 #pragma unroll
         for (int i = 0; i < 64; ++i) {
-            const int v = k0 + i < K ? src[k0 + i] : 0;
+            const long long k = k0 + (i & 31) + (i >> 5) * 128;
+            const int v = k < K ? src[k] : 0;
             const uint32_t b = (v != 0 ? 2u : 0u) | (v < 0 ? 8u : 0u);
             word[i >> 4] |= ((i & 8) ? b >> 1 : b) << (4 * (i & 7));
         }

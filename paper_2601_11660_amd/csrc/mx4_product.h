@@ -1,5 +1,6 @@
 // What the kernels of the microscaled 4-bit products share.
 #pragma once
+#include <utility>
 #include "mx4_common.h"
 
 namespace mbu {
@@ -17,7 +18,84 @@ struct Mx4Args {
 
 enum Mx4Weights { W_HELD, W_MASKED };
 
+constexpr int OUT_OF_RANGE = (int)0x80000000;        // buffer offset beyond every resource: the load returns zeros
+
+__device__ __forceinline__ v4i load16(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
+{
+    return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0));
+}
+__device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
+{
+    return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0);
+}
+// resource over the rows [first, rows) of `pitch` bytes, at most `most` of them; empty where there are none
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void *base, uint32_t first, uint32_t rows, uint32_t most,
+                                                          int pitch)
+{
+    const int bytes = first < rows ? (int)min(rows - first, most) * pitch : 0;
+    return __builtin_amdgcn_make_buffer_rsrc((char *)const_cast<void *>(base) + (uint64_t)first * (uint32_t)pitch, 0, bytes,
+                                             0x00020000);
+}
+
+// f(0), f(1), ... f(N - 1), the number a compile-time constant
+template <typename F, int... I> __device__ __forceinline__ void repeat_each(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void repeat(F &&f)
+{
+    repeat_each(f, std::make_integer_sequence<int, N>());
+}
+
+struct TileAt {
+    int m, n;
+};
+// Blocks are dealt to the eight dies in turn: each die gets a run of tiles of its own, and walks over it in columns
+// of four tiles of rows, so that what its blocks read at one time meets in its cache.
+__device__ __forceinline__ TileAt tile_of_block(int tiles_n, int tiles_m)
+{
+    const int total = gridDim.x, die = blockIdx.x & 7, each = total >> 3, more = total & 7;
+    const int t = die * each + min(die, more) + (blockIdx.x >> 3);
+    const int band = t / (4 * tiles_n), in = t - band * 4 * tiles_n, high = min(4, tiles_m - band * 4);
+    return {band * 4 + in % high, in / high};
+}
+
+// Factor, bias, the one rounding, and the stores of a wave: acc[i][n] holds outputs o + 16 n + 0..3 of row m + 16 i.
+template <int MT, int NT, typename OT>
+__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n, o += 16) {
+        if (o >= (uint32_t)p.N) continue;
+        const int left = (int)min(4u, (uint32_t)p.N - o);
+        v4f alpha = {1, 1, 1, 1}, bias = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < left) {
+                if (p.alpha) alpha[q] = p.alpha[o + q];
+                if (p.bias) bias[q] = p.bias[o + q];
+            }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (m + 16 * i >= (uint32_t)p.M) continue;
+            v4f v = acc[i][n];
+            if (p.alpha) v *= alpha;
+            if (p.bias) v += bias;
+            OT *dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + o;
+            if ((p.N & 3) == 0) mx4_store4(dst, v);
+            else
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (q < left) mx4_store(dst + q, v[q]);
+        }
+    }
+}
+
 // Tiled kernel for many rows (mx4_tile.hip); p.x holds codes
+template <typename OT> struct OutType {};
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<float>, hipStream_t s);
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<_Float16>, hipStream_t s);
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<__bf16>, hipStream_t s);
 int launch_mx4_tile(const char *fn, const Mx4Args &p, bool masked, int dtype, hipStream_t s);
 
 }  // namespace mbu

@@ -4,7 +4,6 @@
 // runs in steps of 512 inputs (mx4_matmul.hip has the assignment of inputs to lanes).  Every wave needs all activations of a
 // step and only its own weights, so the activations (256 bytes of a row per step) go through a double-buffered LDS
 // window, and the weights, which nobody shares, from global memory into the registers of the lane that multiplies them.
-#include <utility>
 #include "mx4_product.h"
 
 namespace mbu {
@@ -12,35 +11,6 @@ namespace mbu {
 // unit of 16 bytes `chunk` of a row of the window; the exclusive or spreads the 16 rows that a quarter of a wave reads
 // over all banks
 __device__ __forceinline__ int window_unit(int row, int chunk) { return row * 16 + (chunk ^ (row & 15)); }
-
-constexpr int OUT_OF_RANGE = (int)0x80000000;        // buffer offset beyond every resource: the load returns zeros
-
-__device__ __forceinline__ v4i load16(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
-{
-    return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0));
-}
-__device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
-{
-    return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0);
-}
-// resource over the rows [first, rows) of `pitch` bytes, at most `most` of them
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void *base, uint32_t first, uint32_t rows, uint32_t most,
-                                                          int pitch)
-{
-    const int bytes = (int)min(rows - first, most) * pitch;
-    return __builtin_amdgcn_make_buffer_rsrc((char *)const_cast<void *>(base) + (uint64_t)first * (uint32_t)pitch, 0, bytes,
-                                             0x00020000);
-}
-
-// f(0), f(1), ... f(N - 1), the number a compile-time constant
-template <typename F, int... I> __device__ __forceinline__ void repeat_each(F &&f, std::integer_sequence<int, I...>)
-{
-    (f(std::integral_constant<int, I>()), ...);
-}
-template <int N, typename F> __device__ __forceinline__ void repeat(F &&f)
-{
-    repeat_each(f, std::make_integer_sequence<int, N>());
-}
 
 // Weights of a wave: SLOTS of 16 bytes per lane and 16 outputs, a slot for one instruction (held) or for two (masked).
 template <Mx4Weights WK, int NT, int SLOTS> struct TileWeights {
@@ -62,13 +32,8 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_kernel(const Mx4Args p)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4, wn = wave & 3, wm = wave >> 2;
 
-    // Blocks are dealt to the eight dies in turn: each die gets a run of tiles of its own, and walks over it in columns
-    // of four tiles of rows, so that what its blocks read at one time meets in its cache.
-    const int tiles_n = p.tiles_n, tiles_m = (int)(((uint32_t)p.M + BM - 1) / BM);
-    const int total = gridDim.x, die = blockIdx.x & 7, each = total >> 3, more = total & 7;
-    const int t = die * each + min(die, more) + (blockIdx.x >> 3);
-    const int band = t / (4 * tiles_n), in = t - band * 4 * tiles_n, high = min(4, tiles_m - band * 4);
-    const int tm = band * 4 + in % high, tn = in / high;
+    const TileAt at_tile = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
+    const int tm = at_tile.m, tn = at_tile.n;
     const uint32_t m0 = (uint32_t)tm * BM, n0 = (uint32_t)tn * BN + wn * 16 * NT;
 
     const int pitch = p.kp >> 1, spitch = p.kp >> 5, steps = p.steps;
@@ -180,33 +145,7 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_kernel(const Mx4Args p)
         __syncthreads();
     }
 
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint32_t o = n0 + 16 * n + 4 * g;
-        if (o >= (uint32_t)p.N) continue;
-        const int left = (int)min(4u, (uint32_t)p.N - o);
-        v4f alpha = {1, 1, 1, 1}, bias = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < left) {
-                if (p.alpha) alpha[q] = p.alpha[o + q];
-                if (p.bias) bias[q] = p.bias[o + q];
-            }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const uint32_t m = m0 + (wm * MT + i) * 16 + r;
-            if (m >= (uint32_t)p.M) continue;
-            v4f v = acc[i][n];
-            if (p.alpha) v *= alpha;
-            if (p.bias) v += bias;
-            OT *dst = (OT *)p.out + (uint64_t)m * (uint32_t)p.N + o;
-            if ((p.N & 3) == 0) mx4_store4(dst, v);
-            else
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (q < left) mx4_store(dst + q, v[q]);
-        }
-    }
+    store_tile<MT, NT, OT>(p, acc, m0 + wm * 16 * MT + r, n0 + 4 * g);
 }
 
 template <Mx4Weights WK, int MW, int MT, int NT, typename OT>
@@ -222,6 +161,7 @@ static int launch_tile(const char *fn, Mx4Args p, hipStream_t s)
 
 template <Mx4Weights WK, typename OT> static int choose_tile(const char *fn, const Mx4Args &p, hipStream_t s)
 {
+    if (WK == W_HELD) return launch_mx4_tile_held(fn, p, OutType<OT>(), s);
     if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_tile<WK, 2, 8, 4, OT>(fn, p, s);
     if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_tile<WK, 1, 8, 2, OT>(fn, p, s);
     return launch_tile<WK, 1, 4, 1, OT>(fn, p, s);

@@ -1,0 +1,171 @@
+// Products in the microscaled 4-bit format for many rows, both operands through LDS.
+//
+// A lane of the matrix instruction holds a row of its own, so neighbouring lanes read different rows: straight from
+// global memory a load of 64 lanes is 64 accesses of the first-level cache instead of 16 (and the weights of a wave took
+// 65 accesses a load, the address unit was busy for 77 % of the time).  Staged through LDS eight lanes read 128
+// consecutive bytes.
+//
+// A block takes 16 MT MW rows by 16 NT NW outputs, a wave 16 MT by 16 NT of them.  Phases of 256 inputs (128 bytes of a row)
+// go through two windows.  In phase t a wave multiplies out of one window; in its first half it writes phase t + 1, which
+// it fetched a phase ago, into the other one, and fetches phase t + 2; a barrier in the middle of the phase makes that
+// window whole, so that the first operands of phase t + 1 are read before phase t ends and no wave waits for them.  The
+// barrier at the start of a phase stands before the writes: by then every wave has multiplied what it read there.
+#include "mx4_product.h"
+
+namespace mbu {
+
+// unit of 16 bytes `chunk` (of eight) of a row of a window: eight rows at one chunk lie in different banks
+__device__ __forceinline__ int phase_unit(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
+
+template <int MW, int NW, int MT, int NT, typename OT>
+__global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_held_kernel(const Mx4Args p)
+{
+    constexpr int BM = 16 * MT * MW, BN = 16 * NT * NW, THREADS = 64 * MW * NW, ROWS = BM + BN;
+    constexpr int UNITS = ROWS * 8 / THREADS, UNITS_A = BM * 8 / THREADS, STRIDE = THREADS / 8;
+    constexpr int SCALES = (ROWS + THREADS - 1) / THREADS;       // rows whose scales a thread stages
+    static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0 && STRIDE % 8 == 0 && MT % 4 == 0 && NT <= 8, "");
+    static_assert(BM % 64 == 0 && THREADS % 64 == 0, "the scales of a wave's threads belong to one operand");
+    __shared__ v4i window[2][ROWS * 8];
+    __shared__ v4i window_scales[2][SCALES * THREADS];           // behind ROWS: zeros, never read
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4, wn = wave % NW, wm = wave / NW;
+    const TileAt at = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
+    const uint32_t m0 = (uint32_t)at.m * BM, n0 = (uint32_t)at.n * BN;
+
+    const int pitch = p.kp >> 1, spitch = p.kp >> 5, steps = p.steps;
+    const __amdgpu_buffer_rsrc_t xr = rows_of(p.x, m0, p.M, BM, pitch), wr = rows_of(p.w, n0, p.N, BN, pitch);
+    // scales: the rows of one operand for each wave
+    __amdgpu_buffer_rsrc_t sr[SCALES];
+#pragma unroll
+    for (int q = 0; q < SCALES; ++q) {
+        const int row = wave * 64 + q * THREADS;                 // the wave's first one
+        const bool x = row < BM;
+        sr[q] = rows_of(x ? p.xs : p.ws, x ? m0 + row : n0 + (row - BM), x ? p.M : p.N, row < ROWS ? 64 : 0, spitch);
+    }
+
+    const int srow = tid >> 3, schunk = tid & 7;                 // what the thread stages: rows srow + STRIDE q
+    const int lane_off = srow * pitch + schunk * 16, write_unit = phase_unit(srow, schunk);
+    const int x_row = wm * 16 * MT + r, w_row = BM + wn * 16 * NT + r;
+    int x_unit[4], w_unit[4];                                    // by instruction of a step: chunk 4 (j & 1) + g
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x_unit[j] = phase_unit(x_row, 4 * (j & 1) + g);
+        w_unit[j] = phase_unit(w_row, 4 * (j & 1) + g);
+    }
+
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = (v4f){0, 0, 0, 0};
+
+    auto fetch = [&](int q, int phase) {
+        const int off = phase * 128 + schunk * 16 < pitch ? lane_off : OUT_OF_RANGE;
+        return q < UNITS_A ? load16(xr, off, q * STRIDE * pitch + phase * 128)
+                           : load16(wr, off, (q - UNITS_A) * STRIDE * pitch + phase * 128);
+    };
+    // the 16 scales of a row's step, in the order in which the lanes take them: word g of the row for lane group g
+    auto fetch_scales = [&](int q, int step) { return load16(sr[q], lane * spitch, step * 16); };
+    auto in_lane_order = [&](v4i s, int step) {
+        s = mx4_row_end(s, spitch - step * 16);
+        return (v4i){(int)mx4_scales_of(s, 0), (int)mx4_scales_of(s, 1), (int)mx4_scales_of(s, 2), (int)mx4_scales_of(s, 3)};
+    };
+
+    v4i st[UNITS], ss[SCALES], f[4], wf[2][NT];
+    uint32_t xs[MT], ws[NT], ws2[NT];
+#pragma unroll
+    for (int q = 0; q < UNITS; ++q) st[q] = fetch(q, 0);
+#pragma unroll
+    for (int q = 0; q < SCALES; ++q) ss[q] = fetch_scales(q, 0);
+#pragma unroll
+    for (int q = 0; q < UNITS; ++q) {
+        window[0][write_unit + q * STRIDE * 8] = st[q];
+        st[q] = fetch(q, 1);
+    }
+#pragma unroll
+    for (int q = 0; q < SCALES; ++q) window_scales[0][q * THREADS + tid] = in_lane_order(ss[q], 0);
+    __syncthreads();
+    const uint32_t *const scales = reinterpret_cast<const uint32_t *>(window_scales);
+    const int xs_at = x_row * 4 + g, ws_at = w_row * 4 + g;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) wf[0][n] = window[0][w_unit[0] + n * 128];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) ws[n] = scales[ws_at + n * 64];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) f[i] = window[0][x_unit[0] + i * 128];
+    xs[0] = scales[xs_at];
+    xs[1] = scales[xs_at + 64];
+
+    for (int step = 0; step < steps; ++step) {
+        const uint32_t *const cur_scales = scales + (step & 1) * (SCALES * THREADS * 4);
+        const uint32_t *const nxt_scales = scales + ((step & 1) ^ 1) * (SCALES * THREADS * 4);
+        repeat<2>([&](auto half) {
+            constexpr int H = decltype(half)::value, GROUPS = 2 * MT, WHOLE = GROUPS - 4;
+            const v4i *const cur = window[H];
+            v4i *const nxt = window[H ^ 1];
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            repeat<GROUPS>([&](auto group) {
+                constexpr int G = decltype(group)::value, i = G % MT, j = 2 * H + G / MT;
+                if constexpr (G == WHOLE) {
+                    __syncthreads();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (G + 3 < GROUPS) f[(G + 3) & 3] = cur[x_unit[(G + 3) / MT] + (G + 3) % MT * 128];
+                else f[(G + 3) & 3] = nxt[x_unit[0] + (G + 3 - GROUPS) * 128];
+                repeat<NT>([&](auto output) {
+                    constexpr int n = decltype(output)::value;
+                    if constexpr (G == n * 4 / (NT > 4 ? NT : 4)) wf[1][n] = cur[w_unit[1] + n * 128];
+                    if constexpr (G == WHOLE + n * 4 / (NT > 4 ? NT : 4)) wf[0][n] = nxt[w_unit[0] + n * 128];
+                    if constexpr (H == 1 && G == WHOLE + n * 4 / (NT > 4 ? NT : 4)) ws2[n] = nxt_scales[ws_at + n * 64];
+                });
+                if constexpr (H == 0 && G + 2 < MT) xs[G + 2] = cur_scales[xs_at + (G + 2) * 64];
+                if constexpr (H == 1 && G >= GROUPS - 2) xs[G - (GROUPS - 2)] = nxt_scales[xs_at + (G - (GROUPS - 2)) * 64];
+                repeat<UNITS>([&](auto unit) {
+                    constexpr int q = decltype(unit)::value;
+                    if constexpr (G == q * WHOLE / UNITS) {
+                        nxt[write_unit + q * STRIDE * 8] = st[q];
+                        st[q] = fetch(q, 2 * step + H + 2);
+                    }
+                });
+                if constexpr (H == 0 && G == MT) {
+#pragma unroll
+                    for (int q = 0; q < SCALES; ++q) ss[q] = fetch_scales(q, step + 1);
+                }
+                if constexpr (H == 1 && G == WHOLE - 2) {
+#pragma unroll
+                    for (int q = 0; q < SCALES; ++q)
+                        window_scales[(step & 1) ^ 1][q * THREADS + tid] = in_lane_order(ss[q], step + 1);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    acc[i][n] = mx4_mfma<j>(wf[G / MT][n], ws[n], f[G & 3], xs[i], acc[i][n]);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+#pragma unroll
+        for (int n = 0; n < NT; ++n) ws[n] = ws2[n];
+    }
+    store_tile<MT, NT, OT>(p, acc, m0 + x_row, n0 + wn * 16 * NT + 4 * g);
+}
+
+template <int MW, int NW, int MT, int NT, typename OT> static int launch_held(const char *fn, Mx4Args p, hipStream_t s)
+{
+    p.tiles_n = ceil_div(p.N, 16 * NT * NW);
+    const long long blocks = (long long)ceil_div(p.M, 16 * MT * MW) * p.tiles_n;
+    if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "%s: product too large", fn);
+    MBU_LAUNCH((mx4_tile_held_kernel<MW, NW, MT, NT, OT>), dim3((unsigned)blocks), dim3(64 * MW * NW), 0, s, p);
+    return check_launch(fn);
+}
+
+template <typename OT> static int choose_held(const char *fn, const Mx4Args &p, hipStream_t s)
+{
+    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_held<2, 4, 8, 4, OT>(fn, p, s);
+    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_held<2, 2, 4, 4, OT>(fn, p, s);
+    return launch_held<1, 4, 4, 1, OT>(fn, p, s);
+}
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<float>, hipStream_t s) { return choose_held<float>(fn, p, s); }
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<_Float16>, hipStream_t s) { return choose_held<_Float16>(fn, p, s); }
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<__bf16>, hipStream_t s) { return choose_held<__bf16>(fn, p, s); }
+
+}  // namespace mbu

@@ -463,7 +463,7 @@ int mbu_mx4_matmul_masked_binary(const uint8_t *a, const uint8_t *a_scales, int 
 /* The layer on float activations: mbu_mx4_quantize on the rows of x, then the product above, in one call.
  *   x          [M] rows of K values of x_dtype, `stride` values apart, aligned to their type only
  *   workspace  at least mbu_mx4_linear_workspace_bytes(M, K) bytes, not shared with a call that may run at the same
- *              time (MBU_ERR_WORKSPACE if smaller); few rows are quantised on the way and leave it untouched */
+ *              time (MBU_ERR_WORKSPACE if smaller); NULL where that is 0: few rows are quantised on the way */
 int mbu_mx4_linear_workspace_bytes(int M, int K, size_t *bytes);
 int mbu_mx4_linear(const void *x, int x_dtype, int M, int K, long long stride, const uint8_t *b,
                    const uint8_t *b_scales, int N, const float *bias, void *out, int dtype, void *workspace,

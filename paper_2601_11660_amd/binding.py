@@ -156,6 +156,10 @@ def _load_native(L: ctypes.CDLL):
             L.mbu_conv3x3_masked_binary, L.mbu_conv3x3_masked_binary_fused, L.mbu_conv3x3_masked_binary_concat,
             L.mbu_conv3x3_masked_binary_two_inputs, L.mbu_tconv2x2_masked_binary, L.mbu_pack_act,
             L.mbu_stem_fp32, L.mbu_classifier_fp32)), torch._C._cuda_getDevice, _raw_stream)
+        native.bind_mx4(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.mbu_mx4_quantize, L.mbu_mx4_dequantize, L.mbu_mx4_matmul, L.mbu_mx4_matmul_masked_binary,
+            L.mbu_mx4_linear, L.mbu_mx4_linear_masked_binary, L.mbu_mx4_linear_workspace_bytes,
+            L.mbu_mx4_packed_masked_binary_bytes)))
         return native
     except (ImportError, OSError) as e:
         warnings.warn(f"{NATIVE_PATH} does not load ({e}): single-layer calls take 2 us longer until it is built "
@@ -531,6 +535,11 @@ def _float_code(dtype: torch.dtype) -> int:
 def mx4_quantize(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """mbu_mx4_quantize: x [rows, K] float32, float16 or bfloat16 -> (codes, scales).  One of x's strides has to be 1
     (a transposed view of a weight stored input-major is read in place)."""
+    r = (_calls or _native()).mx4_quantize(x)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        check(r)
     _here("x", x, _FLOATS, 2)
     rows, k = x.shape
     s0, s1 = x.stride()
@@ -548,6 +557,11 @@ def mx4_quantize(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
 def mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: torch.dtype = torch.float32
                    ) -> torch.Tensor:
     """mbu_mx4_dequantize: the values [rows, k] of held rows."""
+    r = (_calls or _native()).mx4_dequantize(codes, scales, k, dtype)
+    if r.__class__ is torch.Tensor:
+        return r
+    if r is not None:
+        check(r)
     rows, kp = _held("codes", codes, scales)
     if not kp - 128 < k <= kp:
         raise ValueError(f"rows of {kp} codes do not hold {k} values")
@@ -560,6 +574,11 @@ def mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: tor
 def mx4_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
                bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """mbu_mx4_matmul: held rows a [M] and b [N] of the same K -> a b^T + bias, [M, N] of `dtype`."""
+    r = (_calls or _native()).mx4_matmul(a, a_scales, b, b_scales, bias, dtype)
+    if r.__class__ is torch.Tensor:
+        return r
+    if r is not None:
+        check(r)
     m, kp = _held("a", a, a_scales)
     n, kb = _held("b", b, b_scales)
     if kb != kp:
@@ -598,6 +617,11 @@ def mx4_matmul_masked_binary(a: torch.Tensor, a_scales: torch.Tensor, packed: to
                              alpha: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
                              dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """mbu_mx4_matmul_masked_binary: held rows a [M], blob of n outputs -> alpha * (a w^T) + bias, [M, n] of `dtype`."""
+    r = (_calls or _native()).mx4_matmul_masked(a, a_scales, packed, n, alpha, bias, dtype)
+    if r.__class__ is torch.Tensor:
+        return r
+    if r is not None:
+        check(r)
     m, kp = _held("a", a, a_scales)
     code = _float_code(dtype)
     pw = _blob(packed, n, kp)
@@ -617,15 +641,24 @@ def _linear_input(x: torch.Tensor) -> Tuple[int, int, int]:
     return m, k, x.stride(0)
 
 
-def _linear_workspace(m: int, k: int, device) -> torch.Tensor:
+def _linear_workspace(m: int, k: int, device) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """(tensor, address, bytes); no tensor where none is needed."""
     size = ctypes.c_size_t(0)
     check(lib().mbu_mx4_linear_workspace_bytes(m, k, ctypes.byref(size)))
-    return torch.empty(size.value, dtype=torch.uint8, device=device)
+    if not size.value:
+        return None, None, 0
+    t = torch.empty(size.value, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), size.value
 
 
 def mx4_linear(x: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
                dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """mbu_mx4_linear: x [M, K] floats, held weights [N] -> quantised x times b^T + bias, [M, N] of `dtype` (x's)."""
+    r = (_calls or _native()).mx4_linear(x, b, b_scales, bias, dtype)
+    if r.__class__ is torch.Tensor:
+        return r
+    if r is not None:
+        check(r)
     m, k, stride = _linear_input(x)
     n, kp = _held("b", b, b_scales)
     if not kp - 128 < k <= kp:
@@ -633,25 +666,30 @@ def mx4_linear(x: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, bias: O
     dtype = x.dtype if dtype is None else dtype
     code = _float_code(dtype)
     pb = _per_output("bias", bias, n)
-    ws = _linear_workspace(m, k, x.device)
+    _ws, space, size = _linear_workspace(m, k, x.device)
     out = torch.empty((m, n), dtype=dtype, device=x.device)
     check(lib().mbu_mx4_linear(x.data_ptr(), _FLOATS[x.dtype], m, k, stride, b.data_ptr(), b_scales.data_ptr(), n, pb,
-                               out.data_ptr(), code, ws.data_ptr(), ws.numel(), _stream()))
+                               out.data_ptr(), code, space, size, _stream()))
     return out
 
 
 def mx4_linear_masked_binary(x: torch.Tensor, packed: torch.Tensor, n: int, alpha: Optional[torch.Tensor] = None,
                              bias: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """mbu_mx4_linear_masked_binary: the same with masked-binary weights (blob of n outputs) and their factors."""
+    r = (_calls or _native()).mx4_linear_masked(x, packed, n, alpha, bias, dtype)
+    if r.__class__ is torch.Tensor:
+        return r
+    if r is not None:
+        check(r)
     m, k, stride = _linear_input(x)
     dtype = x.dtype if dtype is None else dtype
     code = _float_code(dtype)
     pw = _blob(packed, n, k)
     pa, pb = _per_output("alpha", alpha, n), _per_output("bias", bias, n)
-    ws = _linear_workspace(m, k, x.device)
+    _ws, space, size = _linear_workspace(m, k, x.device)
     out = torch.empty((m, n), dtype=dtype, device=x.device)
     check(lib().mbu_mx4_linear_masked_binary(x.data_ptr(), _FLOATS[x.dtype], m, k, stride, pw, n, pa, pb,
-                                             out.data_ptr(), code, ws.data_ptr(), ws.numel(), _stream()))
+                                             out.data_ptr(), code, space, size, _stream()))
     return out
 
 

@@ -183,14 +183,14 @@ inline Mx4MaskedLayout mx4_masked_layout(int N, int K)
     const int tiles = ceil_div(N, 16), steps = ceil_div(mx4_padded(K), 512);
     return {tiles, steps, (size_t)tiles * steps * 2048};
 }
-// can rows of floats be read 16 bytes at a time?
-inline bool mx4_rows_aligned(const void *x, size_t size, int rows, int K, long long stride)
-{
-    return aligned16(x) && (K * size) % 16 == 0 && (rows == 1 || (stride * (long long)size) % 16 == 0);
-}
 int launch_mx4_quantize(const void *x, int dtype, int rows, int K, long long stride, bool across, uint8_t *codes,
                         uint8_t *scales, hipStream_t s);
 int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype,
+                          hipStream_t s);
+// rows that a product quantises on the way (mx4_few.hip); others are quantised before
+bool mx4_few_floats(int M, int K);
+int launch_mx4_few_floats(const char *fn, const void *x, int x_dtype, int M, long long stride, bool masked, const void *w,
+                          const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
                           hipStream_t s);
 int launch_mx4_pack_masked(const int8_t *w, int N, int K, void *packed, hipStream_t s);
 // masked: w is a blob of masked-binary weights, else codes with scales ws; alpha, bias: float32 [N] or NULL

@@ -94,7 +94,11 @@ static int matmul(const char *fn, const uint8_t *a, const uint8_t *a_scales, int
                              (hipStream_t)stream);
 }
 
-static size_t linear_workspace(int M, int K) { return round_up(code_bytes(M, K), 256) + round_up(scale_bytes(M, K), 256); }
+static size_t linear_workspace(int M, int K)
+{
+    if (mx4_few_floats(M, K)) return 0;
+    return round_up(code_bytes(M, K), 256) + round_up(scale_bytes(M, K), 256);
+}
 
 static int linear(const char *fn, const void *x, int x_dtype, int M, long long stride, const Mx4Product &p,
                   void *workspace, size_t workspace_bytes, void *stream)
@@ -104,8 +108,8 @@ static int linear(const char *fn, const void *x, int x_dtype, int M, long long s
     if (!rc) rc = check_product(fn, M, p);
     if (!rc) rc = check_float_rows(fn, x, x_dtype, M, p.K, stride);
     if (rc) return rc;
-    MBU_REQ_PTR(fn, workspace);
     const size_t need = linear_workspace(M, p.K), n = (size_t)M * p.N * float_size(p.dtype);
+    if (need) MBU_REQ_PTR(fn, workspace);
     if (workspace_bytes < need)
         return fail(MBU_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
     const size_t nx = float_extent(x_dtype, M, p.K, stride);
@@ -114,6 +118,9 @@ static int linear(const char *fn, const void *x, int x_dtype, int M, long long s
         overlap(workspace, need, p.w, nw) || overlap(workspace, need, p.ws, scale_bytes(p.N, p.K)) ||
         overlap(workspace, need, p.alpha, (size_t)p.N * 4) || overlap(workspace, need, p.bias, (size_t)p.N * 4))
         return fail(MBU_ERR_ARG, "%s: output and workspace must not alias an input or each other", fn);
+    if (!need)
+        return launch_mx4_few_floats(fn, x, x_dtype, M, stride, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out,
+                                     p.dtype, (hipStream_t)stream);
     uint8_t *const codes = (uint8_t *)workspace, *const scales = codes + round_up(code_bytes(M, p.K), 256);
     rc = launch_mx4_quantize(x, x_dtype, M, p.K, stride, false, codes, scales, (hipStream_t)stream);
     if (rc) return rc;

@@ -123,6 +123,36 @@ template <> struct Mx4In<_Float16> {
         return q;
     }
 };
+// 16 bytes of a row of floats, aligned to their type only (the hardware takes any address)
+template <typename T> __device__ __forceinline__ uint4 load_floats(const T *p)
+{
+    uint4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+// the first `n` values of a chunk of eight, zeros behind them
+template <typename T> __device__ __forceinline__ Mx4In<T> load_some(const T *p, int n)
+{
+    Mx4In<T> in;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in.set(i, i < n ? p[i] : (T)0.0f);
+    return in;
+}
+template <typename T> __device__ __forceinline__ Mx4In<T> load_eight(const T *p)
+{
+    Mx4In<T> in;
+#pragma unroll
+    for (int c = 0; c < 8 / Mx4In<T>::CHUNK; ++c) in.set_chunk(c, load_floats(p + c * Mx4In<T>::CHUNK));
+    return in;
+}
+template <typename T> __device__ __forceinline__ Mx4In<T> zero_eight()
+{
+    Mx4In<T> in;
+#pragma unroll
+    for (int c = 0; c < 8 / Mx4In<T>::CHUNK; ++c) in.set_chunk(c, make_uint4(0, 0, 0, 0));
+    return in;
+}
+
 // the conversions read the exponent field of the scale alone: 2^-127, whose float32 form is a subnormal, is 0 here
 __device__ __forceinline__ float mx4_scale_float(uint32_t s) { return __uint_as_float(s << 23); }
 

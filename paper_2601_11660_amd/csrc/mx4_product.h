@@ -14,6 +14,7 @@ struct Mx4Args {
     void *out;
     long long ldx;
     int M, N, K, kp, steps, tiles_n;
+    int dtype;                  // of the output
 };
 
 enum Mx4Weights { W_HELD, W_MASKED };
@@ -60,9 +61,8 @@ __device__ __forceinline__ TileAt tile_of_block(int tiles_n, int tiles_m)
     return {band * 4 + in % high, in / high};
 }
 
-// Factor, bias, the one rounding, and the stores of a wave: acc[i][n] holds outputs o + 16 n + 0..3 of row m + 16 i.
 template <int MT, int NT, typename OT>
-__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+__device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
 {
 #pragma unroll
     for (int n = 0; n < NT; ++n, o += 16) {
@@ -90,12 +90,17 @@ __device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT
         }
     }
 }
+// Factor, bias, the one rounding, and the stores of a wave: acc[i][n] holds outputs o + 16 n + 0..3 of row m + 16 i.
+template <int MT, int NT>
+__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+{
+    if (p.dtype == MBU_FLOAT32) store_as<MT, NT, float>(p, acc, m, o);
+    else if (p.dtype == MBU_FLOAT16) store_as<MT, NT, _Float16>(p, acc, m, o);
+    else store_as<MT, NT, __bf16>(p, acc, m, o);
+}
 
-// Tiled kernel for many rows (mx4_tile.hip); p.x holds codes
-template <typename OT> struct OutType {};
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<float>, hipStream_t s);
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<_Float16>, hipStream_t s);
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<__bf16>, hipStream_t s);
-int launch_mx4_tile(const char *fn, const Mx4Args &p, bool masked, int dtype, hipStream_t s);
+// Tiled kernels for many rows (mx4_tile_held.hip, mx4_tile_masked.hip); p.x holds codes
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, hipStream_t s);
+int launch_mx4_tile_masked(const char *fn, const Mx4Args &p, hipStream_t s);
 
 }  // namespace mbu

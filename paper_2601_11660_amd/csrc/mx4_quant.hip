@@ -5,10 +5,10 @@ namespace mbu {
 
 // Rows with consecutive values.  Eight values a thread, so four threads share a block's scale (two lane exchanges
 // inside a quad); `tpr` threads (a power of two) walk along a row, UNROLL groups of eight each with all loads in flight.
-// VEC: rows start on 16 bytes and K is a multiple of what 16 bytes hold.
+// Rows are read 16 bytes at a time wherever they start; WHOLE: K is a multiple of eight.
 constexpr int QUANT_UNROLL = 4;
 
-template <typename T, bool VEC>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T *__restrict__ x, long long stride, int rows, int K,
                                                            int kp, int tpr_log, int segs, uint8_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales)
@@ -23,18 +23,9 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T *__restrict__
 #pragma unroll
     for (int u = 0; u < QUANT_UNROLL; ++u) {
         const int k = (first + u * tpr) * 8;
-        if (VEC) {
-            constexpr int C = Mx4In<T>::CHUNK;
-#pragma unroll
-            for (int c = 0; c < 8 / C; ++c) {
-                uint4 w = {0, 0, 0, 0};
-                if (k + c * C < K) w = *reinterpret_cast<const uint4 *>(src + k + c * C);
-                in[u].set_chunk(c, w);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) in[u].set(i, k + i < K ? src[k + i] : (T)0.0f);
-        }
+        in[u] = zero_eight<T>();
+        if (k + 8 <= K) in[u] = load_eight(src + k);
+        else if (!WHOLE && k < K) in[u] = load_some(src + k, K - k);
     }
 #pragma unroll
     for (int u = 0; u < QUANT_UNROLL; ++u) {
@@ -179,7 +170,7 @@ static int quantize(const T *x, int rows, int K, long long stride, bool across, 
     const int rc = quant_geometry(rows, kp / 8, &lg, &segs, &blocks);
     if (rc) return rc;
     const dim3 grid((unsigned)blocks), block(256);
-    if (mx4_rows_aligned(x, sizeof(T), rows, K, stride))
+    if (K % 8 == 0)
         MBU_LAUNCH((mx4_quantize_kernel<T, true>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);
     else
         MBU_LAUNCH((mx4_quantize_kernel<T, false>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);

@@ -17,7 +17,7 @@ namespace mbu {
 // unit of 16 bytes `chunk` (of eight) of a row of a window: eight rows at one chunk lie in different banks
 __device__ __forceinline__ int phase_unit(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
 
-template <int MW, int NW, int MT, int NT, typename OT>
+template <int MW, int NW, int MT, int NT>
 __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_held_kernel(const Mx4Args p)
 {
     constexpr int BM = 16 * MT * MW, BN = 16 * NT * NW, THREADS = 64 * MW * NW, ROWS = BM + BN;
@@ -146,26 +146,23 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
 #pragma unroll
         for (int n = 0; n < NT; ++n) ws[n] = ws2[n];
     }
-    store_tile<MT, NT, OT>(p, acc, m0 + x_row, n0 + wn * 16 * NT + 4 * g);
+    store_tile<MT, NT>(p, acc, m0 + x_row, n0 + wn * 16 * NT + 4 * g);
 }
 
-template <int MW, int NW, int MT, int NT, typename OT> static int launch_held(const char *fn, Mx4Args p, hipStream_t s)
+template <int MW, int NW, int MT, int NT> static int launch_held(const char *fn, Mx4Args p, hipStream_t s)
 {
     p.tiles_n = ceil_div(p.N, 16 * NT * NW);
     const long long blocks = (long long)ceil_div(p.M, 16 * MT * MW) * p.tiles_n;
     if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "%s: product too large", fn);
-    MBU_LAUNCH((mx4_tile_held_kernel<MW, NW, MT, NT, OT>), dim3((unsigned)blocks), dim3(64 * MW * NW), 0, s, p);
+    MBU_LAUNCH((mx4_tile_held_kernel<MW, NW, MT, NT>), dim3((unsigned)blocks), dim3(64 * MW * NW), 0, s, p);
     return check_launch(fn);
 }
 
-template <typename OT> static int choose_held(const char *fn, const Mx4Args &p, hipStream_t s)
+int launch_mx4_tile_held(const char *fn, const Mx4Args &p, hipStream_t s)
 {
-    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_held<2, 4, 8, 4, OT>(fn, p, s);
-    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_held<2, 2, 4, 4, OT>(fn, p, s);
-    return launch_held<1, 4, 4, 1, OT>(fn, p, s);
+    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_held<2, 4, 8, 4>(fn, p, s);
+    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_held<2, 2, 4, 4>(fn, p, s);
+    return launch_held<1, 4, 4, 1>(fn, p, s);
 }
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<float>, hipStream_t s) { return choose_held<float>(fn, p, s); }
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<_Float16>, hipStream_t s) { return choose_held<_Float16>(fn, p, s); }
-int launch_mx4_tile_held(const char *fn, const Mx4Args &p, OutType<__bf16>, hipStream_t s) { return choose_held<__bf16>(fn, p, s); }
 
 }  // namespace mbu

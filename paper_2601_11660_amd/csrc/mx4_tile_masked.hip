@@ -1,0 +1,134 @@
+// Products of activations in the microscaled 4-bit format with masked-binary weights, for many rows: activations through
+// LDS, weights straight into registers.
+//
+// A block takes 16 MT MW rows by 4 x 16 NT outputs, a wave 16 MT by 16 NT of them.  The sum runs in steps of 512 inputs.
+// The activations of a step (256 bytes of a row) are shared by the waves and go through a double-buffered LDS window; the
+// weights lie in the order in which the lanes read them, two bits each, and need no window: a load of 16 bytes per lane
+// is one run of 1 KB and feeds two matrix instructions after a shift and two masks.
+#include "mx4_product.h"
+
+namespace mbu {
+
+// unit of 16 bytes `chunk` of a row of the window; the exclusive or spreads the 16 rows that a quarter of a wave reads
+// over all banks
+__device__ __forceinline__ int window_unit(int row, int chunk) { return row * 16 + (chunk ^ (row & 15)); }
+
+template <int MW, int MT, int NT>
+__global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4Args p)
+{
+    constexpr int BM = 16 * MT * MW, BN = 64 * NT, THREADS = 256 * MW;
+    __shared__ v4i window[2][BM * 16];
+    __shared__ v4i window_scales[2][THREADS];                    // rows behind BM: zeros, never read
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4, wn = wave & 3, wm = wave >> 2;
+
+    const TileAt at_tile = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
+    const int tm = at_tile.m, tn = at_tile.n;
+    const uint32_t m0 = (uint32_t)tm * BM, n0 = (uint32_t)tn * BN + wn * 16 * NT;
+
+    const int pitch = p.kp >> 1, spitch = p.kp >> 5, steps = p.steps;
+    const __amdgpu_buffer_rsrc_t xr = rows_of(p.x, m0, p.M, BM, pitch), xsr = rows_of(p.xs, m0, p.M, BM, spitch);
+    const uint32_t nw = min(n0, (uint32_t)p.N - 1);              // a wave behind the last output: nothing is stored
+    const uint32_t tiles_w = ((uint32_t)p.N + 15) / 16;
+    const __amdgpu_buffer_rsrc_t wr = rows_of(p.w, nw / 16, tiles_w, NT, steps * 2048);
+
+    const int srow = tid >> 4, schunk = tid & 15;                // what the thread stages: rows srow + 16 MW q
+    const int x_lane = srow * pitch + schunk * 16, xs_lane = tid < BM ? tid * spitch : OUT_OF_RANGE;
+    const int write_unit = window_unit(srow, schunk);
+    const int read_row = wm * 16 * MT + r;
+    int read_unit[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) read_unit[j] = window_unit(read_row, 4 * j + g);
+
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = (v4f){0, 0, 0, 0};
+
+    v4i w[2][NT];                                                // half a step's weights: instructions 0, 1 and 2, 3
+    auto load_weights = [&](int half, int step) {
+        const int off = step < steps ? lane * 16 : OUT_OF_RANGE;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w[half][n] = load16(wr, off, (n * steps + step) * 2048 + half * 1024);
+    };
+    auto weight = [&](int j, int n) {
+        const v4i v = w[j >> 1][n];
+        return (j & 1) ? expand_masked((uint32_t)v.z, (uint32_t)v.w) : expand_masked((uint32_t)v.x, (uint32_t)v.y);
+    };
+    constexpr uint32_t ONE = 0x7f7f7f7fu;                        // scales 2^0
+    auto stage = [&](int q, int step) {
+        const int off = step * 256 + schunk * 16 < pitch ? x_lane : OUT_OF_RANGE;
+        return load16(xr, off, q * 16 * MW * pitch + step * 256);
+    };
+    // the scales of one row, in the order in which the lanes take them: word g of a row for lane group g
+    auto stage_scales = [&](int step) { return load16(xsr, xs_lane, step * 16); };
+    auto in_lane_order = [&](v4i s, int step) {
+        s = mx4_row_end(s, spitch - step * 16);
+        return (v4i){(int)mx4_scales_of(s, 0), (int)mx4_scales_of(s, 1), (int)mx4_scales_of(s, 2), (int)mx4_scales_of(s, 3)};
+    };
+
+    {
+        v4i st[MT];
+#pragma unroll
+        for (int q = 0; q < MT; ++q) st[q] = stage(q, 0);
+        const v4i ss = stage_scales(0);
+        load_weights(0, 0);
+        load_weights(1, 0);
+#pragma unroll
+        for (int q = 0; q < MT; ++q) window[0][write_unit + q * 256 * MW] = st[q];
+        window_scales[0][tid] = in_lane_order(ss, 0);
+    }
+    __syncthreads();
+
+    for (int step = 0; step < steps; ++step) {
+        const v4i *cur = window[step & 1];
+        const uint32_t *cur_scales = reinterpret_cast<const uint32_t *>(window_scales[step & 1]) + read_row * 4 + g;
+        v4i *nxt = window[(step & 1) ^ 1];
+        uint32_t xs[MT];
+        v4i st[MT], f[4], ss;
+        constexpr int GROUPS = 4 * MT, EVERY = MT >= 8 ? 3 : 2, BEHIND = GROUPS - EVERY * MT;
+        xs[0] = cur_scales[0];
+        if (MT > 1) xs[1] = cur_scales[64];
+        repeat<3>([&](auto group) {
+            constexpr int G = decltype(group)::value;
+            f[G] = cur[read_unit[G / MT] + (G % MT) * 256];
+        });
+        repeat<GROUPS>([&](auto group) {
+            constexpr int G = decltype(group)::value, j = G / MT, i = G % MT;
+            if constexpr (G + 3 < GROUPS) f[(G + 3) & 3] = cur[read_unit[(G + 3) / MT] + ((G + 3) % MT) * 256];
+            if constexpr (G + 2 < MT) xs[G + 2] = cur_scales[(G + 2) * 64];
+            if constexpr (G % EVERY == 0 && G / EVERY < MT) st[G / EVERY] = stage(G / EVERY, step + 1);
+            if constexpr (G == MT) ss = stage_scales(step + 1);
+            if constexpr (G >= BEHIND && (G - BEHIND) % EVERY == 0 && (G - BEHIND) / EVERY < MT)
+                nxt[write_unit + (G - BEHIND) / EVERY * 256 * MW] = st[(G - BEHIND) / EVERY];
+            if constexpr (G == GROUPS - 1) window_scales[(step & 1) ^ 1][tid] = in_lane_order(ss, step + 1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                acc[i][n] = mx4_mfma<j>(weight(j, n), ONE, f[G & 3], xs[i], acc[i][n]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (i == MT - 1 && (j & 1)) load_weights(j >> 1, step + 1);
+        });
+        __syncthreads();
+    }
+
+    store_tile<MT, NT>(p, acc, m0 + wm * 16 * MT + r, n0 + 4 * g);
+}
+
+template <int MW, int MT, int NT> static int launch_masked(const char *fn, Mx4Args p, hipStream_t s)
+{
+    p.tiles_n = ceil_div(p.N, 64 * NT);
+    const long long blocks = (long long)ceil_div(p.M, 16 * MT * MW) * p.tiles_n;
+    if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "%s: product too large", fn);
+    MBU_LAUNCH((mx4_tile_masked_kernel<MW, MT, NT>), dim3((unsigned)blocks), dim3(256 * MW), 0, s, p);
+    return check_launch(fn);
+}
+
+int launch_mx4_tile_masked(const char *fn, const Mx4Args &p, hipStream_t s)
+{
+    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_masked<2, 8, 4>(fn, p, s);
+    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_masked<1, 8, 2>(fn, p, s);
+    return launch_masked<1, 4, 1>(fn, p, s);
+}
+
+}  // namespace mbu

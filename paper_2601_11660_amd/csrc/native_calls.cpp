@@ -11,6 +11,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/device_lazy_init.h>
@@ -28,6 +29,14 @@ struct {
     decltype(&mbu_pack_act) pack;
     decltype(&mbu_stem_fp32) stem;
     decltype(&mbu_classifier_fp32) classifier;
+    decltype(&mbu_mx4_quantize) quantize;
+    decltype(&mbu_mx4_dequantize) dequantize;
+    decltype(&mbu_mx4_matmul) matmul;
+    decltype(&mbu_mx4_matmul_masked_binary) matmul_masked;
+    decltype(&mbu_mx4_linear) linear;
+    decltype(&mbu_mx4_linear_masked_binary) linear_masked;
+    decltype(&mbu_mx4_linear_workspace_bytes) linear_workspace;
+    decltype(&mbu_mx4_packed_masked_binary_bytes) masked_bytes;
     PyObject *device, *stream;
 } g;
 
@@ -265,6 +274,292 @@ PyObject *classifier(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- microscaled 4-bit operators: as above, and every tensor on the current device
+
+// type code of the C ABI, -1 for another type
+int float_code(at::ScalarType t)
+{
+    return t == at::kFloat ? MBU_FLOAT32 : t == at::kHalf ? MBU_FLOAT16 : t == at::kBFloat16 ? MBU_BFLOAT16 : -1;
+}
+
+// a dense matrix or vector of the plain kind, whatever its strides
+const at::Tensor *dense(PyObject *o, int dim)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const DispatchKeySet known({DispatchKey::CUDA, DispatchKey::ADInplaceOrView, DispatchKey::AutogradCUDA,
+                                DispatchKey::AutocastCUDA});
+    return t.defined() && t.is_cuda() && (t.key_set().raw_repr() & ~known.raw_repr()) == 0 && t.dim() == dim && sizes_fit(t)
+               ? &t : nullptr;
+}
+
+struct Held {
+    const uint8_t *codes, *scales;
+    int rows, kp;
+    c10::Device device = c10::Device(c10::kCPU);
+};
+// codes [rows, Kp / 2] and scales [rows, Kp / 32]
+bool held(PyObject *codes, PyObject *scales, Held &h)
+{
+    const at::Tensor *c = plain(codes, at::kByte, 2), *s = plain(scales, at::kByte, 2);
+    if (!c || !s || c->dim() != 2 || s->dim() != 2 || !sizes_fit(*c) || c->device() != s->device()) return false;
+    const int64_t rows = c->size(0), kp = 2 * c->size(1);
+    if (kp % 128 || kp > 0x7fffffffLL || s->size(0) != rows || s->size(1) != kp / 32) return false;
+    h.codes = pointer<uint8_t>(*c);
+    h.scales = pointer<uint8_t>(*s);
+    h.rows = (int)rows;
+    h.kp = (int)kp;
+    h.device = c->device();
+    return true;
+}
+
+// None, or float32 of n values
+bool per_output(PyObject *o, int64_t n, c10::Device device, const float *&p)
+{
+    p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = plain(o, at::kFloat, 1);
+    if (!t || t->dim() != 1 || t->size(0) != n || t->device() != device) return false;
+    p = pointer<float>(*t);
+    return true;
+}
+
+bool blob(PyObject *o, int n, int k, c10::Device device, const void *&p)
+{
+    const at::Tensor *t = plain(o, at::kByte, 1);
+    size_t bytes = 0;
+    if (!t || t->dim() != 1 || t->device() != device || g.masked_bytes(n, k, &bytes) != MBU_OK ||
+        (uint64_t)t->numel() != bytes)
+        return false;
+    p = pointer<uint8_t>(*t);
+    return true;
+}
+
+// the current stream, if the current device is `device`
+bool stream_of(const at::Tensor &t, void *&s)
+{
+    torch::utils::maybe_initialize_device(t.device());
+    PyObject *d = PyObject_CallNoArgs(g.device);
+    if (!d) throw python_error();
+    const long index = PyLong_AsLong(d);
+    if (index != t.device().index()) {
+        Py_DECREF(d);
+        if (index == -1 && PyErr_Occurred()) throw python_error();
+        return false;
+    }
+    PyObject *r = PyObject_CallOneArg(g.stream, d);
+    Py_DECREF(d);
+    if (!r) throw python_error();
+    s = PyLong_AsVoidPtr(r);
+    Py_DECREF(r);
+    if (!s && PyErr_Occurred()) throw python_error();
+    return true;
+}
+
+struct Floats {
+    const void *p;
+    int rows, k, code;
+    int64_t s0, s1;
+    at::ScalarType type;
+    c10::Device device;
+    explicit Floats(const at::Tensor &t)
+        : p(t.data_ptr()), rows((int)t.size(0)), k((int)t.size(1)), code(float_code(t.scalar_type())), s0(t.stride(0)),
+          s1(t.stride(1)), type(t.scalar_type()), device(t.device())
+    {
+    }
+};
+
+// (x) -> (codes, scales)
+PyObject *mx4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    if (n != 1 || !g.stream || !ordinary()) Py_RETURN_NONE;
+    const at::Tensor *t = dense(a[0], 2);
+    if (!t || float_code(t->scalar_type()) < 0 || !stream_of(*t, s)) Py_RETURN_NONE;
+    const Floats x(*t);
+    const bool across = x.k > 1 && x.s1 != 1;
+    if (across && x.rows > 1 && x.s0 != 1) Py_RETURN_NONE;
+    at::Tensor codes, scales;
+    const int rc = unlocked([&] {
+        const int64_t kp = (x.k + 127LL) / 128 * 128;
+        codes = make({x.rows, kp / 2}, at::kByte, x.device);
+        scales = make({x.rows, kp / 32}, at::kByte, x.device);
+        return g.quantize(x.p, x.code, x.rows, x.k, across ? x.s1 : x.s0, across ? 1 : 0, (uint8_t *)codes.data_ptr(),
+                          (uint8_t *)scales.data_ptr(), s);
+    });
+    return result(rc, codes, scales);
+    END_HANDLE_TH_ERRORS
+}
+
+bool out_type(PyObject *o, at::ScalarType &t)
+{
+    if (!THPDtype_Check(o)) return false;
+    t = ((THPDtype *)o)->scalar_type;
+    return float_code(t) >= 0;
+}
+
+// (codes, scales, k, dtype) -> values
+PyObject *mx4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    Held h;
+    int k;
+    at::ScalarType type;
+    if (n != 4 || !g.stream || !ordinary() || !held(a[0], a[1], h) || !whole(a[2], k) || !out_type(a[3], type) ||
+        k > h.kp || k <= h.kp - 128 || !stream_of(THPVariable_Unpack(a[0]), s))
+        Py_RETURN_NONE;
+    at::Tensor out;
+    const int rc = unlocked([&] {
+        out = make({h.rows, k}, type, h.device);
+        return g.dequantize(h.codes, h.scales, h.rows, k, out.data_ptr(), float_code(type), s);
+    });
+    return result(rc, out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (a, a_scales, b, b_scales, bias, dtype) -> a b^T + bias
+PyObject *mx4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    Held x, w;
+    const float *bias;
+    at::ScalarType type;
+    if (n != 6 || !g.stream || !ordinary() || !held(a[0], a[1], x) || !held(a[2], a[3], w) || x.kp != w.kp ||
+        x.device != w.device || !per_output(a[4], w.rows, x.device, bias) || !out_type(a[5], type) ||
+        !stream_of(THPVariable_Unpack(a[0]), s))
+        Py_RETURN_NONE;
+    at::Tensor out;
+    const int rc = unlocked([&] {
+        out = make({x.rows, w.rows}, type, x.device);
+        return g.matmul(x.codes, x.scales, x.rows, w.codes, w.scales, w.rows, x.kp, bias, out.data_ptr(), float_code(type), s);
+    });
+    return result(rc, out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (a, a_scales, packed, outputs, alpha, bias, dtype) -> alpha * (a w^T) + bias
+PyObject *mx4_matmul_masked(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    Held x;
+    int outputs;
+    const void *packed;
+    const float *alpha, *bias;
+    at::ScalarType type;
+    if (n != 7 || !g.stream || !ordinary() || !held(a[0], a[1], x) || !whole(a[3], outputs) ||
+        !blob(a[2], outputs, x.kp, x.device, packed) || !per_output(a[4], outputs, x.device, alpha) ||
+        !per_output(a[5], outputs, x.device, bias) || !out_type(a[6], type) || !stream_of(THPVariable_Unpack(a[0]), s))
+        Py_RETURN_NONE;
+    at::Tensor out;
+    const int rc = unlocked([&] {
+        out = make({x.rows, outputs}, type, x.device);
+        return g.matmul_masked(x.codes, x.scales, x.rows, packed, outputs, x.kp, alpha, bias, out.data_ptr(),
+                               float_code(type), s);
+    });
+    return result(rc, out);
+    END_HANDLE_TH_ERRORS
+}
+
+// float rows for the two linear calls, and the type of the output (None: that of x)
+const at::Tensor *linear_input(PyObject *x, PyObject *dtype, at::ScalarType &type)
+{
+    const at::Tensor *t = dense(x, 2);
+    if (!t || float_code(t->scalar_type()) < 0 || (t->size(1) > 1 && t->stride(1) != 1)) return nullptr;
+    type = t->scalar_type();
+    return dtype == Py_None || out_type(dtype, type) ? t : nullptr;
+}
+// its workspace; undefined where none is needed
+int linear_space(const Floats &x, at::Tensor &ws, size_t &bytes)
+{
+    const int rc = g.linear_workspace(x.rows, x.k, &bytes);
+    if (rc == MBU_OK && bytes) ws = make({(int64_t)bytes}, at::kByte, x.device);
+    return rc;
+}
+
+// (x, b, b_scales, bias, dtype) -> quantised x times b^T + bias
+PyObject *mx4_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    Held w;
+    const float *bias;
+    at::ScalarType type;
+    if (n != 5 || !g.stream || !ordinary()) Py_RETURN_NONE;
+    const at::Tensor *t = linear_input(a[0], a[4], type);
+    if (!t || !held(a[1], a[2], w) || w.device != t->device() || t->size(1) > w.kp || t->size(1) <= w.kp - 128 ||
+        !per_output(a[3], w.rows, w.device, bias) || !stream_of(*t, s))
+        Py_RETURN_NONE;
+    const Floats x(*t);
+    at::Tensor out, ws;
+    const int rc = unlocked([&] {
+        size_t bytes = 0;
+        out = make({x.rows, w.rows}, type, x.device);
+        const int e = linear_space(x, ws, bytes);
+        return e ? e : g.linear(x.p, x.code, x.rows, x.k, x.s0, w.codes, w.scales, w.rows, bias, out.data_ptr(),
+                                float_code(type), bytes ? ws.data_ptr() : nullptr, bytes, s);
+    });
+    return result(rc, out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, packed, outputs, alpha, bias, dtype) -> alpha * (quantised x times w^T) + bias
+PyObject *mx4_linear_masked(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    void *s;
+    int outputs;
+    const void *packed;
+    const float *alpha, *bias;
+    at::ScalarType type;
+    if (n != 6 || !g.stream || !ordinary()) Py_RETURN_NONE;
+    const at::Tensor *t = linear_input(a[0], a[5], type);
+    if (!t || !whole(a[2], outputs) || !blob(a[1], outputs, (int)t->size(1), t->device(), packed) ||
+        !per_output(a[3], outputs, t->device(), alpha) || !per_output(a[4], outputs, t->device(), bias) ||
+        !stream_of(*t, s))
+        Py_RETURN_NONE;
+    const Floats x(*t);
+    at::Tensor out, ws;
+    const int rc = unlocked([&] {
+        size_t bytes = 0;
+        out = make({x.rows, outputs}, type, x.device);
+        const int e = linear_space(x, ws, bytes);
+        return e ? e : g.linear_masked(x.p, x.code, x.rows, x.k, x.s0, packed, outputs, alpha, bias, out.data_ptr(),
+                                       float_code(type), bytes ? ws.data_ptr() : nullptr, bytes, s);
+    });
+    return result(rc, out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (addresses of the eight C-ABI functions of these operators in the order of `g`)
+PyObject *bind_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[8];
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "bind_mx4: eight addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 8; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_mx4: null address");
+            return nullptr;
+        }
+    }
+    g.quantize = (decltype(g.quantize))p[0];
+    g.dequantize = (decltype(g.dequantize))p[1];
+    g.matmul = (decltype(g.matmul))p[2];
+    g.matmul_masked = (decltype(g.matmul_masked))p[3];
+    g.linear = (decltype(g.linear))p[4];
+    g.linear_masked = (decltype(g.linear_masked))p[5];
+    g.linear_workspace = (decltype(g.linear_workspace))p[6];
+    g.masked_bytes = (decltype(g.masked_bytes))p[7];
+    Py_RETURN_NONE;
+}
+
 // (addresses of the eight C-ABI functions in the order of `g`, current device, current raw stream of a device)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -298,6 +593,9 @@ PyMethodDef methods[] = {
     MBU_METHOD("bind", bind), MBU_METHOD("conv", conv), MBU_METHOD("fused", two_inputs<FUSED>),
     MBU_METHOD("concat", two_inputs<CONCAT>), MBU_METHOD("two_inputs", two_inputs<TWO>), MBU_METHOD("tconv", tconv),
     MBU_METHOD("pack", pack), MBU_METHOD("stem", stem), MBU_METHOD("classifier", classifier),
+    MBU_METHOD("bind_mx4", bind_mx4), MBU_METHOD("mx4_quantize", mx4_quantize), MBU_METHOD("mx4_dequantize", mx4_dequantize),
+    MBU_METHOD("mx4_matmul", mx4_matmul), MBU_METHOD("mx4_matmul_masked", mx4_matmul_masked),
+    MBU_METHOD("mx4_linear", mx4_linear), MBU_METHOD("mx4_linear_masked", mx4_linear_masked),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

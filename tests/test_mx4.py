@@ -70,20 +70,21 @@ def test_linear_refuses():
     n = ctypes.c_size_t()
     assert L.mbu_mx4_linear_workspace_bytes(3, 100, None) == B.MBU_ERR_NULL
     assert L.mbu_mx4_linear_workspace_bytes(0, 100, ctypes.byref(n)) == B.MBU_ERR_SHAPE
-    assert L.mbu_mx4_linear_workspace_bytes(3, 100, ctypes.byref(n)) == 0 and n.value >= 3 * (64 + 4)
+    assert L.mbu_mx4_linear_workspace_bytes(3, 100, ctypes.byref(n)) == 0 and n.value == 0     # quantised on the way
+    assert L.mbu_mx4_linear_workspace_bytes(100, 100, ctypes.byref(n)) == 0 and n.value >= 100 * (64 + 4)
     need = n.value
     f = L.mbu_mx4_linear
-    assert f(None, 0, 3, 100, 100, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_NULL
-    assert f(X, 0, 3, 100, 100, W, WS, 8, V, O, 0, None, need, None) == B.MBU_ERR_NULL
-    assert f(X, 0, 3, 100, 100, W, WS, 8, V, O, 0, WK, need - 1, None) == B.MBU_ERR_WORKSPACE
-    assert f(X, 4, 3, 100, 100, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_ARG
-    assert f(X, 0, 3, 100, -1, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_SHAPE
-    assert f(X, 0, 3, 100, 100, W, WS, 8, V, O, 0, WK + 8, need, None) == B.MBU_ERR_ALIGN
-    for out, ws in ((X, WK), (O, X), (O, O), (O, W), (O, V), (X + 1184, WK)):
-        assert f(X, 0, 3, 100, 100, W, WS, 8, V, out, 0, ws, need, None) == B.MBU_ERR_ARG
+    assert f(None, 0, 100, 100, 100, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_NULL
+    assert f(X, 0, 100, 100, 100, W, WS, 8, V, O, 0, None, need, None) == B.MBU_ERR_NULL
+    assert f(X, 0, 100, 100, 100, W, WS, 8, V, O, 0, WK, need - 1, None) == B.MBU_ERR_WORKSPACE
+    assert f(X, 4, 100, 100, 100, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_ARG
+    assert f(X, 0, 100, 100, -1, W, WS, 8, V, O, 0, WK, need, None) == B.MBU_ERR_SHAPE
+    assert f(X, 0, 100, 100, 100, W, WS, 8, V, O, 0, WK + 8, need, None) == B.MBU_ERR_ALIGN
+    for out, ws in ((X, WK), (O, X), (O, O), (O, W), (O, V), (X + 39984, WK)):
+        assert f(X, 0, 100, 100, 100, W, WS, 8, V, out, 0, ws, need, None) == B.MBU_ERR_ARG
     g = L.mbu_mx4_linear_masked_binary
-    assert g(X, 0, 3, 100, 100, None, 8, V, None, O, 0, WK, need, None) == B.MBU_ERR_NULL
-    assert g(X, 0, 3, 100, 100, W, 8, V, None, O, 0, WK, 0, None) == B.MBU_ERR_WORKSPACE
+    assert g(X, 0, 100, 100, 100, None, 8, V, None, O, 0, WK, need, None) == B.MBU_ERR_NULL
+    assert g(X, 0, 100, 100, 100, W, 8, V, None, O, 0, WK, 0, None) == B.MBU_ERR_WORKSPACE
 
 
 def test_packed_masked_binary_size():

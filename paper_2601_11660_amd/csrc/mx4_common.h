@@ -183,6 +183,12 @@ __device__ __forceinline__ v4i expand_masked(uint32_t w0, uint32_t w1)
     return r;
 }
 
+// the type that a template argument of mbu_float_type stands for
+template <int CODE> struct Mx4Type { using T = uint8_t; };
+template <> struct Mx4Type<MBU_FLOAT32> { using T = float; };
+template <> struct Mx4Type<MBU_FLOAT16> { using T = _Float16; };
+template <> struct Mx4Type<MBU_BFLOAT16> { using T = __bf16; };
+
 // The one rounding of a product: from the float32 sum to the output's type, to nearest even.
 __device__ __forceinline__ void mx4_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void mx4_store(__bf16 *p, float v) { *p = (__bf16)v; }

@@ -17,7 +17,8 @@ struct Mx4Args {
     int dtype;                  // of the output
 };
 
-enum Mx4Weights { W_HELD, W_MASKED };
+// template arguments that name a type: those of mbu_float_type, or held codes
+constexpr int HELD = 3;
 
 constexpr int OUT_OF_RANGE = (int)0x80000000;        // buffer offset beyond every resource: the load returns zeros
 

@@ -8,8 +8,8 @@ namespace mbu {
 // Rows are read 16 bytes at a time wherever they start; WHOLE: K is a multiple of eight.
 constexpr int QUANT_UNROLL = 4;
 
-template <typename T, bool WHOLE>
-__global__ __launch_bounds__(256) void mx4_quantize_kernel(const T *__restrict__ x, long long stride, int rows, int K,
+template <int TYPE, bool WHOLE>
+__global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restrict__ values, long long stride, int rows, int K,
                                                            int kp, int tpr_log, int segs, uint8_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales)
 {
@@ -18,7 +18,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T *__restrict__
     const long long row = (long long)group * (256 >> tpr_log) + (threadIdx.x >> tpr_log);
     if (row >= rows) return;                       // whole quads: tpr is a multiple of 16
     const int first = seg * tpr * QUANT_UNROLL + (threadIdx.x & (tpr - 1));
-    const T *src = x + row * stride;
+    using T = typename Mx4Type<TYPE>::T;
+    const T *src = (const T *)values + row * stride;
     Mx4In<T> in[QUANT_UNROLL];
 #pragma unroll
     for (int u = 0; u < QUANT_UNROLL; ++u) {
@@ -44,8 +45,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T *__restrict__
 
 // Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes one block of its row, 64
 // consecutive rows per wave.
-template <typename T>
-__global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const T *__restrict__ x, long long stride, int rows,
+template <int TYPE>
+__global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__restrict__ values, long long stride, int rows,
                                                                   int K, int kp, int kgroups,
                                                                   uint8_t *__restrict__ codes,
                                                                   uint8_t *__restrict__ scales)
@@ -55,6 +56,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const T *__res
     const long long row = (long long)tile * 64 + lane;
     if (row >= rows) return;
     const int k0 = kg * 128 + wave * 32;
+    using T = typename Mx4Type<TYPE>::T;
+    const T *const x = (const T *)values;
     Mx4In<T> in[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -87,10 +90,10 @@ __device__ __forceinline__ void mx4_values(uint32_t q, uint32_t s, float v[8])
     }
 }
 
-template <typename T, bool VEC>
+template <int TYPE, bool VEC>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes,
                                                              const uint8_t *__restrict__ scales, int rows, int K, int kp,
-                                                             int tpr_log, int segs, T *__restrict__ out)
+                                                             int tpr_log, int segs, void *__restrict__ out)
 {
     const int tpr = 1 << tpr_log;
     const int group = blockIdx.x / segs, seg = blockIdx.x - group * segs;
@@ -105,7 +108,8 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
         const uint32_t s = scales[row * (kp >> 5) + (k >> 5)];
         float v[8];
         mx4_values(q, s, v);
-        T *dst = out + row * K + k;
+        using T = typename Mx4Type<TYPE>::T;
+        T *dst = (T *)out + row * K + k;
         if (VEC) {
             mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
             mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
@@ -152,8 +156,8 @@ static int quant_geometry(int rows, int per_row, int *tpr_log, int *segs, long l
     return *blocks <= 0x7fffffffLL ? MBU_OK : fail(MBU_ERR_SHAPE, "mbu_mx4: tensor too large");
 }
 
-template <typename T>
-static int quantize(const T *x, int rows, int K, long long stride, bool across, uint8_t *codes, uint8_t *scales,
+template <int TYPE>
+static int quantize(const void *x, int rows, int K, long long stride, bool across, uint8_t *codes, uint8_t *scales,
                     hipStream_t s)
 {
     const int kp = mx4_padded(K);
@@ -161,7 +165,7 @@ static int quantize(const T *x, int rows, int K, long long stride, bool across, 
         const int kg = kp / 128;
         const long long blocks = ((long long)rows + 63) / 64 * kg;
         if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_quantize: tensor too large");
-        MBU_LAUNCH((mx4_quantize_across_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, x, stride, rows, K, kp, kg,
+        MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, x, stride, rows, K, kp, kg,
                    codes, scales);
         return check_launch("mbu_mx4_quantize");
     }
@@ -171,22 +175,22 @@ static int quantize(const T *x, int rows, int K, long long stride, bool across, 
     if (rc) return rc;
     const dim3 grid((unsigned)blocks), block(256);
     if (K % 8 == 0)
-        MBU_LAUNCH((mx4_quantize_kernel<T, true>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);
+        MBU_LAUNCH((mx4_quantize_kernel<TYPE, true>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);
     else
-        MBU_LAUNCH((mx4_quantize_kernel<T, false>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);
+        MBU_LAUNCH((mx4_quantize_kernel<TYPE, false>), grid, block, 0, s, x, stride, rows, K, kp, lg, segs, codes, scales);
     return check_launch("mbu_mx4_quantize");
 }
 
 int launch_mx4_quantize(const void *x, int dtype, int rows, int K, long long stride, bool across, uint8_t *codes,
                         uint8_t *scales, hipStream_t s)
 {
-    if (dtype == MBU_FLOAT32) return quantize((const float *)x, rows, K, stride, across, codes, scales, s);
-    if (dtype == MBU_FLOAT16) return quantize((const _Float16 *)x, rows, K, stride, across, codes, scales, s);
-    return quantize((const __bf16 *)x, rows, K, stride, across, codes, scales, s);
+    if (dtype == MBU_FLOAT32) return quantize<MBU_FLOAT32>(x, rows, K, stride, across, codes, scales, s);
+    if (dtype == MBU_FLOAT16) return quantize<MBU_FLOAT16>(x, rows, K, stride, across, codes, scales, s);
+    return quantize<MBU_BFLOAT16>(x, rows, K, stride, across, codes, scales, s);
 }
 
-template <typename T>
-static int dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, T *out, hipStream_t s)
+template <int TYPE>
+static int dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, hipStream_t s)
 {
     const int kp = mx4_padded(K);
     int lg, segs;
@@ -195,18 +199,18 @@ static int dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int
     if (rc) return rc;
     const dim3 grid((unsigned)blocks), block(256);
     if (K % 8 == 0)
-        MBU_LAUNCH((mx4_dequantize_kernel<T, true>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
+        MBU_LAUNCH((mx4_dequantize_kernel<TYPE, true>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
     else
-        MBU_LAUNCH((mx4_dequantize_kernel<T, false>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
+        MBU_LAUNCH((mx4_dequantize_kernel<TYPE, false>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
     return check_launch("mbu_mx4_dequantize");
 }
 
 int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype,
                           hipStream_t s)
 {
-    if (dtype == MBU_FLOAT32) return dequantize(codes, scales, rows, K, (float *)out, s);
-    if (dtype == MBU_FLOAT16) return dequantize(codes, scales, rows, K, (_Float16 *)out, s);
-    return dequantize(codes, scales, rows, K, (__bf16 *)out, s);
+    if (dtype == MBU_FLOAT32) return dequantize<MBU_FLOAT32>(codes, scales, rows, K, out, s);
+    if (dtype == MBU_FLOAT16) return dequantize<MBU_FLOAT16>(codes, scales, rows, K, out, s);
+    return dequantize<MBU_BFLOAT16>(codes, scales, rows, K, out, s);
 }
 
 int launch_mx4_pack_masked(const int8_t *w, int N, int K, void *packed, hipStream_t s)

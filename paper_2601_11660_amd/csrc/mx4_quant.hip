@@ -43,38 +43,88 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restric
     }
 }
 
-// Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes one block of its row, 64
-// consecutive rows per wave.
+// Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes blocks of its own rows, one of
+// float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four waves take eight
+// consecutive blocks of these rows and put the codes together in LDS, so that 128 consecutive bytes of a row are
+// written at a time; written by the lanes, 16 bytes here and there, 8192 x 8192 of bfloat16 took 76 us.
+constexpr int ACROSS_K = 256;
+template <int TYPE> struct AcrossRows {
+    static constexpr int PER_LANE = TYPE == MBU_FLOAT32 ? 1 : 2;
+    static constexpr int ROWS = 64 * PER_LANE;
+};
+
 template <int TYPE>
-__global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__restrict__ values, long long stride, int rows,
-                                                                  int K, int kp, int kgroups,
+__global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__restrict__ values, long long stride,
+                                                                  int rows, int K, int kp, int kgroups,
                                                                   uint8_t *__restrict__ codes,
                                                                   uint8_t *__restrict__ scales)
 {
+    using T = typename Mx4Type<TYPE>::T;
+    constexpr int PER_LANE = AcrossRows<TYPE>::PER_LANE, ROWS = AcrossRows<TYPE>::ROWS;
+    __shared__ uint4 code_tile[ROWS][9];                       // an odd number of units apart
+    __shared__ uint8_t scale_tile[ROWS][8];
     const int tile = blockIdx.x / kgroups, kg = blockIdx.x - tile * kgroups;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long row = (long long)tile * 64 + lane;
-    if (row >= rows) return;
-    const int k0 = kg * 128 + wave * 32;
-    using T = typename Mx4Type<TYPE>::T;
-    const T *const x = (const T *)values;
-    Mx4In<T> in[4];
+    const long long row0 = (long long)tile * ROWS, row = row0 + lane * PER_LANE;
+    // no branch around the loads, so that all are under way together: lanes behind the last row read rows that exist
+    const long long from = max(0ll, min(row, (long long)rows - PER_LANE));
+    const T *const x = (const T *)values + from;
+    const bool odd = PER_LANE == 2 && row == from + 1;         // the last row alone: the upper half of what was read
+    const bool single = PER_LANE == 2 && rows == 1;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int turn = 0; turn < 2; ++turn) {
+        const int block = turn * 4 + wave, k0 = kg * ACROSS_K + block * 32;
+        uint32_t v[32];
+        if (!single) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int k = k0 + 8 * j + i;
-            in[j].set(i, k < K ? x[k * stride + row] : (T)0.0f);
+            for (int i = 0; i < 32; ++i) __builtin_memcpy(&v[i], x + min(k0 + i, K - 1) * stride, 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                uint16_t one;
+                __builtin_memcpy(&one, x + min(k0 + i, K - 1) * stride, 2);
+                v[i] = one;
+            }
         }
-    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) top = max(top, in[j].top());
-    const uint32_t s = mx4_scale_byte(top);
-    uint32_t q[4];
+        for (int i = 0; i < 32; ++i) v[i] = k0 + i < K ? odd ? v[i] >> 16 : v[i] : 0u;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = s == 255u ? 0u : in[j].codes(mx4_scale_float(s));
-    *reinterpret_cast<uint4 *>(codes + row * (kp >> 1) + (k0 >> 1)) = make_uint4(q[0], q[1], q[2], q[3]);
-    scales[row * (kp >> 5) + (k0 >> 5)] = (uint8_t)s;
+        for (int e = 0; e < PER_LANE; ++e) {
+            Mx4In<T> in[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8 / PER_LANE; ++i)       // two 16-bit values of one row side by side
+                    in[j].v[i] = PER_LANE == 1 ? v[8 * j + i]
+                                               : __builtin_amdgcn_perm(v[8 * j + 2 * i + 1], v[8 * j + 2 * i],
+                                                                       e ? 0x07060302u : 0x05040100u);
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, in[j].top());
+            const uint32_t s = mx4_scale_byte(top);
+            const float scale = mx4_scale_float(s);
+            uint32_t q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = s == 255u ? 0u : in[j].codes(scale);
+            code_tile[lane * PER_LANE + e][block] = make_uint4(q[0], q[1], q[2], q[3]);
+            scale_tile[lane * PER_LANE + e][block] = (uint8_t)s;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ROWS * 8 / 256; ++u) {
+        const int at = u * 256 + threadIdx.x, r = at >> 3, b = at & 7, k = kg * ACROSS_K + b * 32;
+        if (row0 + r < rows && k < kp)
+            *reinterpret_cast<uint4 *>(codes + (row0 + r) * (kp >> 1) + (k >> 1)) = code_tile[r][b];
+    }
+    // four scales at a time: a row holds a multiple of four
+#pragma unroll
+    for (int u = 0; u < (ROWS * 2 + 255) / 256; ++u) {
+        const int at = u * 256 + threadIdx.x, r = at >> 1, b = (at & 1) * 4, k = kg * ACROSS_K + b * 32;
+        if (r < ROWS && row0 + r < rows && k < kp)
+            *reinterpret_cast<uint32_t *>(scales + (row0 + r) * (kp >> 5) + (k >> 5)) =
+                *reinterpret_cast<const uint32_t *>(&scale_tile[r][b]);
+    }
 }
 
 // number of codes [8 i, 8 i + 8) -> values; every product of a code and a scale is exact in float32
@@ -90,33 +140,100 @@ __device__ __forceinline__ void mx4_values(uint32_t q, uint32_t s, float v[8])
     }
 }
 
-template <int TYPE, bool VEC>
+// K a multiple of what 16 bytes of output hold: a thread writes 16 bytes.
+template <int TYPE>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes,
                                                              const uint8_t *__restrict__ scales, int rows, int K, int kp,
                                                              int tpr_log, int segs, void *__restrict__ out)
 {
+    using T = typename Mx4Type<TYPE>::T;
+    constexpr int EACH = 16 / sizeof(T);
     const int tpr = 1 << tpr_log;
     const int group = blockIdx.x / segs, seg = blockIdx.x - group * segs;
     const long long row = (long long)group * (256 >> tpr_log) + (threadIdx.x >> tpr_log);
     if (row >= rows) return;
     const int first = seg * tpr * QUANT_UNROLL + (threadIdx.x & (tpr - 1));
+    uint32_t q[QUANT_UNROLL], s[QUANT_UNROLL];
 #pragma unroll
     for (int u = 0; u < QUANT_UNROLL; ++u) {
-        const int k = (first + u * tpr) * 8;
-        if (k >= K) break;
-        const uint32_t q = *reinterpret_cast<const uint32_t *>(codes + row * (kp >> 1) + (k >> 1));
-        const uint32_t s = scales[row * (kp >> 5) + (k >> 5)];
-        float v[8];
-        mx4_values(q, s, v);
-        using T = typename Mx4Type<TYPE>::T;
-        T *dst = (T *)out + row * K + k;
-        if (VEC) {
-            mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
-            mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
-        } else {
+        const int k = min((first + u * tpr) * EACH, K - EACH);
+        const uint8_t *const at = codes + row * (kp >> 1) + (k >> 1);
+        q[u] = EACH == 8 ? *reinterpret_cast<const uint32_t *>(at) : *reinterpret_cast<const uint16_t *>(at);
+        s[u] = scales[row * (kp >> 5) + (k >> 5)];
+    }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < K) mx4_store(dst + i, v[i]);
+    for (int u = 0; u < QUANT_UNROLL; ++u) {
+        const int k = (first + u * tpr) * EACH;
+        float v[8];
+        mx4_values(q[u], s[u], v);
+        if (k >= K) break;
+        T *const dst = (T *)out + row * K + k;
+        mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
+        if (EACH == 8) mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
+    }
+}
+
+// Any K: rows of the output start anywhere, so the output is taken as one array and a thread writes 16 aligned bytes of
+// it.  Its values are consecutive nibbles of one row, of at most two blocks, and of the next row's first block where the
+// row ends among them (K < 8: value by value).
+template <int TYPE>
+__global__ __launch_bounds__(256) void mx4_dequantize_ragged_kernel(const uint8_t *__restrict__ codes,
+                                                                    const uint8_t *__restrict__ scales, int K, int kp,
+                                                                    long long total, void *__restrict__ out)
+{
+    using T = typename Mx4Type<TYPE>::T;
+    constexpr int EACH = 16 / sizeof(T);
+    const long long first = (long long)blockIdx.x * (256 * EACH * QUANT_UNROLL);   // the block's first value
+    const long long row0 = total >> 32 ? first / K : (uint32_t)first / (uint32_t)K;
+    auto scale_of = [](uint32_t s) {                                          // 2^-127 is a subnormal, 255 a NaN
+        return __uint_as_float(s == 255u ? 0x7fc00000u : s == 0u ? 0x00400000u : s << 23);
+    };
+#pragma unroll
+    for (int u = 0; u < QUANT_UNROLL; ++u) {
+        const uint32_t k0 = (uint32_t)(first - row0 * K) + (u * 256 + threadIdx.x) * EACH;
+        const uint32_t down = k0 / (uint32_t)K;
+        const int k = (int)(k0 - down * (uint32_t)K);
+        const long long row = row0 + down, at = first + (u * 256 + threadIdx.x) * EACH;
+        if (at >= total) return;
+        T *const dst = (T *)out + at;
+        if (K >= EACH) {
+            const long long below = at + (K - k) < total ? row + 1 : row;       // the next row, if there is one
+            const uint8_t *const c = codes + row * (kp >> 1), *const sc = scales + row * (kp >> 5);
+            const int byte = min(k >> 1, (kp >> 1) - 8), here = min(EACH, K - k), last = min(k + EACH, K) - 1;
+            uint64_t w;
+            uint32_t next;
+            __builtin_memcpy(&w, c + byte, 8);
+            __builtin_memcpy(&next, codes + below * (kp >> 1), 4);
+            const float s0 = scale_of(sc[k >> 5]), s1 = scale_of(sc[last >> 5]), s2 = scale_of(scales[below * (kp >> 5)]);
+            uint32_t q = (uint32_t)(w >> (8 * ((k >> 1) - byte) + 4 * (k & 1)));
+            if (here < 8) q = (q & ((1u << 4 * here) - 1u)) | next << 4 * here;
+            const int same = 32 - (k & 31);                                   // values of the first block
+            const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                v[i] = (i & 1 ? p[i >> 1].y : p[i >> 1].x) * (i >= here ? s2 : i < same ? s0 : s1);
+            if (at + EACH <= total) {
+                mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
+                if (EACH == 8) mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
+            } else {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (at + i < total) mx4_store(dst + i, v[i]);
+            }
+            continue;
+        }
+        long long r = row;
+        int c = k;
+        for (int i = 0; i < EACH && at + i < total; ++i) {
+            const uint32_t byte = codes[r * (kp >> 1) + (c >> 1)];
+            const v2f p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c & 1 ? byte >> 4 : byte, 1.0f, 0);
+            mx4_store(dst + i, p.x * scale_of(scales[r * (kp >> 5) + (c >> 5)]));
+            if (++c == K) {
+                c = 0;
+                ++r;
+            }
         }
     }
 }
@@ -162,8 +279,8 @@ static int quantize(const void *x, int rows, int K, long long stride, bool acros
 {
     const int kp = mx4_padded(K);
     if (across) {
-        const int kg = kp / 128;
-        const long long blocks = ((long long)rows + 63) / 64 * kg;
+        const int kg = ceil_div(kp, ACROSS_K);
+        const long long blocks = ((long long)rows + AcrossRows<TYPE>::ROWS - 1) / AcrossRows<TYPE>::ROWS * kg;
         if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_quantize: tensor too large");
         MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, x, stride, rows, K, kp, kg,
                    codes, scales);
@@ -192,16 +309,19 @@ int launch_mx4_quantize(const void *x, int dtype, int rows, int K, long long str
 template <int TYPE>
 static int dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, hipStream_t s)
 {
+    constexpr int EACH = TYPE == MBU_FLOAT32 ? 4 : 8;
     const int kp = mx4_padded(K);
-    int lg, segs;
-    long long blocks;
-    const int rc = quant_geometry(rows, ceil_div(K, 8), &lg, &segs, &blocks);
-    if (rc) return rc;
-    const dim3 grid((unsigned)blocks), block(256);
-    if (K % 8 == 0)
-        MBU_LAUNCH((mx4_dequantize_kernel<TYPE, true>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
-    else
-        MBU_LAUNCH((mx4_dequantize_kernel<TYPE, false>), grid, block, 0, s, codes, scales, rows, K, kp, lg, segs, out);
+    if (K % EACH == 0) {
+        int lg, segs;
+        long long blocks;
+        const int rc = quant_geometry(rows, K / EACH, &lg, &segs, &blocks);
+        if (rc) return rc;
+        MBU_LAUNCH((mx4_dequantize_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, rows, K, kp, lg, segs, out);
+    } else {
+        const long long total = (long long)rows * K, per = 256 * EACH * QUANT_UNROLL, blocks = (total + per - 1) / per;
+        if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_dequantize: tensor too large");
+        MBU_LAUNCH((mx4_dequantize_ragged_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, K, kp, total, out);
+    }
     return check_launch("mbu_mx4_dequantize");
 }
 

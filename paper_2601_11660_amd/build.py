@@ -30,6 +30,8 @@ EXTRA_FLAGS = {
     # the first layer reads its few accumulators straight back with vector instructions:
     # keep them in ordinary vector registers instead of accumulation registers
     "stem_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    # few accumulators beside many operands: some of both went through accumulation registers and back
+    "mx4_wave.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

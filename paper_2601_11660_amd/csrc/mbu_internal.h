@@ -187,15 +187,8 @@ int launch_mx4_quantize(const void *x, int dtype, int rows, int K, long long str
                         uint8_t *scales, hipStream_t s);
 int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int K, void *out, int dtype,
                           hipStream_t s);
-// rows that a product quantises on the way (mx4_few.hip); others are quantised before
-bool mx4_few_floats(int M, int K);
-int launch_mx4_few_floats(const char *fn, const void *x, int x_dtype, int M, long long stride, bool masked, const void *w,
-                          const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
-                          hipStream_t s);
+bool mx4_few_fits(int M, int K);         // does the kernel for few rows take such a product?
+bool mx4_few_floats(int M, int K);       // does a product quantise such rows on the way?
 int launch_mx4_pack_masked(const int8_t *w, int N, int K, void *packed, hipStream_t s);
-// masked: w is a blob of masked-binary weights, else codes with scales ws; alpha, bias: float32 [N] or NULL
-int launch_mx4_matmul(const char *fn, const uint8_t *a, const uint8_t *as, int M, bool masked, const void *w,
-                      const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
-                      hipStream_t s);
 
 }  // namespace mbu

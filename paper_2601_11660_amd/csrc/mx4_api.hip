@@ -1,5 +1,5 @@
 // C-ABI entry points of the microscaled 4-bit operators: argument checks and dispatch.
-#include "mx4_common.h"
+#include "mx4_product.h"
 
 namespace mbu {
 
@@ -56,6 +56,23 @@ struct Mx4Product {
     int dtype;
 };
 
+static Mx4Args arguments(const Mx4Product &p, const void *x, const uint8_t *xs, long long ldx, int M)
+{
+    const int kp = mx4_padded(p.K);
+    return {x, xs, p.w, p.ws, p.alpha, p.bias, p.out, ldx, M, p.N, p.K, kp, ceil_div(kp, 512), 0, p.dtype};
+}
+
+// Rows in the format.  One token up to 16: every weight is read once and that is all there is to it (16 x 4096 x 4096: 4.2
+// us, in tiles of 32 rows 5.0).  Up to a tile of 64 x 64 for each compute unit the waves of a block share the inputs, beyond
+// that the rows and outputs (777 x 1001 x 2050, 208 tiles: 8.2 and 9.4 us; 512 x 4096 x 4096, 512 tiles: 16.8 and 11.8).
+static int multiply(const char *fn, const Mx4Product &p, const uint8_t *x, const uint8_t *xs, int M, hipStream_t s)
+{
+    const Mx4Args a = arguments(p, x, xs, 0, M);
+    if (mx4_few_fits(M, p.K)) return launch_mx4_few(fn, a, HELD, p.masked, s);
+    if ((long long)ceil_div(M, 64) * ceil_div(p.N, 64) <= 256) return launch_mx4_wave(fn, a, p.masked, s);
+    return p.masked ? launch_mx4_tile_masked(fn, a, s) : launch_mx4_tile_held(fn, a, s);
+}
+
 // what the two forms of the product and the two of the linear layer have in common
 static int check_product(const char *fn, int M, const Mx4Product &p)
 {
@@ -90,8 +107,7 @@ static int matmul(const char *fn, const uint8_t *a, const uint8_t *a_scales, int
     const size_t n = (size_t)M * p.N * float_size(p.dtype);
     if (overlap(p.out, n, a, code_bytes(M, p.K)) || overlap(p.out, n, a_scales, scale_bytes(M, p.K)))
         return fail(MBU_ERR_ARG, "%s: the output must not alias an input", fn);
-    return launch_mx4_matmul(fn, a, a_scales, M, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out, p.dtype,
-                             (hipStream_t)stream);
+    return multiply(fn, p, a, a_scales, M, (hipStream_t)stream);
 }
 
 static size_t linear_workspace(int M, int K)
@@ -119,13 +135,11 @@ static int linear(const char *fn, const void *x, int x_dtype, int M, long long s
         overlap(workspace, need, p.alpha, (size_t)p.N * 4) || overlap(workspace, need, p.bias, (size_t)p.N * 4))
         return fail(MBU_ERR_ARG, "%s: output and workspace must not alias an input or each other", fn);
     if (!need)
-        return launch_mx4_few_floats(fn, x, x_dtype, M, stride, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out,
-                                     p.dtype, (hipStream_t)stream);
+        return launch_mx4_few(fn, arguments(p, x, nullptr, stride, M), x_dtype, p.masked, (hipStream_t)stream);
     uint8_t *const codes = (uint8_t *)workspace, *const scales = codes + round_up(code_bytes(M, p.K), 256);
     rc = launch_mx4_quantize(x, x_dtype, M, p.K, stride, false, codes, scales, (hipStream_t)stream);
     if (rc) return rc;
-    return launch_mx4_matmul(fn, codes, scales, M, p.masked, p.w, p.ws, p.N, p.K, p.alpha, p.bias, p.out, p.dtype,
-                             (hipStream_t)stream);
+    return multiply(fn, p, codes, scales, M, (hipStream_t)stream);
 }
 
 }  // namespace mbu

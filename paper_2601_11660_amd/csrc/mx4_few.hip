@@ -2,28 +2,45 @@
 //
 // A block's waves share the steps of 512 inputs and take the same 16 outputs, so that even one token on a small layer
 // keeps every compute unit busy; they add their sums up in LDS, in the waves' order, and go on to the next 16 outputs
-// while the weights of those are on their way already.  The rows stay in registers as fragments, quantised there where
-// they come as floats: a lane owns whole blocks of 32, so nothing crosses lanes.
+// while the weights of those are on their way already.  The rows stay in registers as fragments; floats are quantised by
+// the block on the way.
 #include "mx4_product.h"
 
 namespace mbu {
 
 constexpr int FEW_WAVES = 16;
 
+// buffers of the waves' sums: one where two and the windows would not fit into LDS
+__host__ __device__ constexpr int few_sums(bool windows, int sw) { return windows && sw > 1 ? 1 : 2; }
+
 struct Mx4Frag {
     v4i c[4];
     uint32_t s;
 };
 
-// 512 inputs of one held row for the lane's group; zeros where the row has ended
-__device__ __forceinline__ void load_held(Mx4Frag &f, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales, int row,
-                                          int pitch, int spitch, int step, int g)
+// 512 inputs of sixteen held rows by way of a window in LDS of the wave's own: sixteen lanes fetch 256 consecutive bytes of
+// a row (the exclusive or spreads what is read at one place of sixteen rows over the banks), four lanes its scales.
+// Behind the last row and the rows' end are zeros.
+constexpr int FEW_WINDOW = 16 * 16 + 16;
+
+__device__ __forceinline__ void fetch_rows(v4i *window, const void *codes, const uint8_t *scales, uint32_t first,
+                                           uint32_t rows, int pitch, int spitch, int step, int lane)
+{
+    const __amdgpu_buffer_rsrc_t cr = rows_of(codes, first, rows, 16, pitch), sr = rows_of(scales, first, rows, 16, spitch);
+    const int row = lane >> 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int at = ((lane & 15) ^ (4 * q + row)) * 16;
+        load_to_lds(cr, window + q * 64, step * 256 + at < pitch ? row * pitch + at : OUT_OF_RANGE, q * 4 * pitch + step * 256);
+    }
+    load4_to_lds(sr, window + 256, step * 16 + (lane & 3) * 4 < spitch ? (lane >> 2) * spitch + (lane & 3) * 4 : OUT_OF_RANGE,
+                 step * 16);
+}
+__device__ __forceinline__ void take_rows(v4i (&c)[4], v4i &s, const v4i *window, int r, int g)
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        f.c[j] = load16(codes, step * 256 + j * 64 < pitch ? row * pitch + g * 16 : OUT_OF_RANGE, step * 256 + j * 64);
-    const v4i s = load16(scales, step * 16 < spitch ? row * spitch : OUT_OF_RANGE, step * 16);
-    f.s = mx4_scales_of(mx4_row_end(s, spitch - step * 16), g);
+    for (int j = 0; j < 4; ++j) c[j] = window[r * 16 + ((4 * j + g) ^ r)];
+    s = window[256 + r];
 }
 
 // Rows of K floats (aligned to their type only), quantised by the whole block into LDS: a thread takes 32 consecutive
@@ -70,6 +87,7 @@ template <typename T> struct FewItem {
 template <bool MASKED> struct FewWeights;
 template <> struct FewWeights<false> {
     v4i c[4], s;
+    // Straight into the registers: the shortest way, but as a lane holds a row, every lane is an access of its own.
     __device__ __forceinline__ void load(const Mx4Args &p, int tile, int step, int lane)
     {
         const int pitch = p.kp >> 1, spitch = p.kp >> 5, r = lane & 15, g = lane >> 4;
@@ -103,39 +121,41 @@ template <> struct FewWeights<true> {
     __device__ __forceinline__ uint32_t scales(const Mx4Args &, int, int) const { return 0x7f7f7f7fu; }
 };
 
-// X: type of the rows, HELD or that of floats.  MT: 16 rows each.  SW: steps of a wave at most, with the rows' fragments kept in
-// registers; 0: any number, the rows read again for every 16 outputs.
-template <int X, bool MASKED, int MT, int SW>
+// Up to 16 rows.  X: their type, HELD or that of floats.  SW: steps of a wave at most.
+template <int X, bool MASKED, int SW>
 __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p)
 {
-    // first the quantised rows, then the waves' sums [2][wave][MT][64 lanes]
+    // first the quantised rows, then the waves' sums [SUMS][wave][64 lanes] and windows
     extern __shared__ v4i shared[];
-    v4f *const part = reinterpret_cast<v4f *>(shared);
+    constexpr bool WINDOWS = !MASKED || X == HELD;
+    constexpr int SUMS = few_sums(WINDOWS, SW);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int r = lane & 15, g = lane >> 4, pitch = p.kp >> 1, spitch = p.kp >> 5, tiles = p.tiles_n;
-    constexpr int KEPT = SW ? SW : 1;
+    v4f *const part = reinterpret_cast<v4f *>(shared);
+    v4i *const window = shared + SUMS * waves * 64 + wave * (SW * FEW_WINDOW);
 
     using XT = typename Mx4Type<X>::T;
-    FewWeights<MASKED> w[KEPT];
-    Mx4Frag x[MT][KEPT];
+    FewWeights<MASKED> w[SW];
+    Mx4Frag x[SW];
     auto load_weights = [&](int k, int tile) { w[k].load(p, tile, wave + k * waves, lane); };
-    auto load_rows = [&](int k, int step) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-            load_held(x[i][k], rows_of(p.x, 0, p.M, 16 * MT, pitch), rows_of(p.xs, 0, p.M, 16 * MT, spitch),
-                      min(16 * i + r, p.M - 1), pitch, spitch, step, g);
-    };
 
     int tile = blockIdx.x;
     // the rows before the weights: they come from the cache, and loads return in order
-    if constexpr (X == HELD && SW) {
+    if constexpr (X == HELD) {
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k) {
-            load_rows(k, wave + k * waves);
+        for (int k = 0; k < SW; ++k) {
+            fetch_rows(window + k * FEW_WINDOW, p.x, p.xs, 0, p.M, pitch, spitch, wave + k * waves, lane);
             load_weights(k, tile);
         }
-    }
-    if constexpr (X != HELD) {
+        __builtin_amdgcn_s_waitcnt(VM_0);                          // what was fetched into the windows is there
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < SW; ++k) {
+            v4i s;
+            take_rows(x[k].c, s, window + k * FEW_WINDOW, r, g);
+            x[k].s = mx4_scales_of(s, g);
+        }
+    } else {
         uint8_t *const codes = reinterpret_cast<uint8_t *>(shared), *const scales = codes + p.M * few_code_pitch(p.steps);
         const int items = p.M * p.steps * 16;
         constexpr int TOGETHER = sizeof(XT) == 4 ? 1 : 2;
@@ -150,7 +170,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
         };
         fetch(threadIdx.x);
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k) load_weights(k, tile);
+        for (int k = 0; k < SW; ++k) load_weights(k, tile);
         quantize();
         for (int at = threadIdx.x + TOGETHER * blockDim.x; at < items; at += TOGETHER * blockDim.x) {
             fetch(at);
@@ -159,117 +179,96 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
         __syncthreads();
         const int row = min(r, p.M - 1);
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k) {
+        for (int k = 0; k < SW; ++k) {
             const int step = min(wave + k * waves, p.steps - 1);
             const v4i *const c = reinterpret_cast<const v4i *>(codes + row * few_code_pitch(p.steps) + step * 256);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[0][k].c[j] = c[j * 4 + g];
-            x[0][k].s = mx4_scales_of(*reinterpret_cast<const v4i *>(scales + row * few_scale_pitch(p.steps) + step * 16), g);
+            for (int j = 0; j < 4; ++j) x[k].c[j] = c[j * 4 + g];
+            x[k].s = mx4_scales_of(*reinterpret_cast<const v4i *>(scales + row * few_scale_pitch(p.steps) + step * 16), g);
         }
         __syncthreads();
     }
     for (int turn = 0; tile < tiles; ++turn) {
         const int next = tile + gridDim.x;
-        v4f acc[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i] = (v4f){0, 0, 0, 0};
+        v4f acc = {0, 0, 0, 0};
         auto multiply = [&](int k, int step) {
             const uint32_t s = w[k].scales(p, step, g);
             repeat<4>([&](auto number) {
                 constexpr int j = decltype(number)::value;
-                const v4i c = w[k].codes(j);
-#pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i] = mx4_mfma<j>(c, s, x[i][k].c[j], x[i][k].s, acc[i]);
+                acc = mx4_mfma<j>(w[k].codes(j), s, x[k].c[j], x[k].s, acc);
             });
         };
-        if (SW) {
+        if constexpr (!MASKED)
+            if (turn) {
+                __builtin_amdgcn_s_waitcnt(VM_0);                  // what was fetched into the windows is there
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < KEPT; ++k) {
-                multiply(k, wave + k * waves);
-                load_weights(k, next);
+                for (int k = 0; k < SW; ++k) take_rows(w[k].c, w[k].s, window + k * FEW_WINDOW, r, g);
             }
-        } else {
-            for (int step = wave; step < p.steps; step += waves) {
-                w[0].load(p, tile, step, lane);
-                load_rows(0, step);
-                multiply(0, step);
-            }
+#pragma unroll
+        for (int k = 0; k < SW; ++k) {
+            multiply(k, wave + k * waves);
+            if (MASKED) load_weights(k, next);
         }
+        part[((turn % SUMS) * waves + wave) * 64 + lane] = acc;
+        if constexpr (!MASKED)
+            if (next < tiles) {
+                __builtin_amdgcn_sched_barrier(0);                 // the operands are out of the windows: they are multiplied
 #pragma unroll
-        for (int i = 0; i < MT; ++i) part[(((turn & 1) * waves + wave) * MT + i) * 64 + lane] = acc[i];
+                for (int k = 0; k < SW; ++k)
+                    fetch_rows(window + k * FEW_WINDOW, p.w, p.ws, (uint32_t)next * 16, p.N, pitch, spitch, wave + k * waves, lane);
+            }
         __syncthreads();
         // the waves take turns at adding up
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-            if ((turn * MT + i) % waves == wave) {
-                const v4f *const sums = part + (((turn & 1) * waves) * MT + i) * 64 + lane;
-                v4f v[1][1] = {{sums[0]}};
-                for (int s = 1; s < waves; ++s) v[0][0] += sums[s * MT * 64];
-                store_tile<1, 1>(p, v, 16 * i + r, (uint32_t)tile * 16 + 4 * g);
-            }
+        if (turn % waves == wave) {
+            const v4f *const sums = part + (turn % SUMS) * waves * 64 + lane;
+            v4f v[1][1] = {{sums[0]}};
+            for (int s = 1; s < waves; ++s) v[0][0] += sums[s * 64];
+            store_tile<1, 1>(p, v, r, (uint32_t)tile * 16 + 4 * g);
+        }
+        if (SUMS == 1) __syncthreads();
         tile = next;
     }
 }
 
-template <int X, bool MASKED, int MT, int SW> static int launch_few(const char *fn, Mx4Args p, hipStream_t s)
+template <int X, bool MASKED, int SW> static int launch_few(const char *fn, Mx4Args p, hipStream_t s)
 {
     p.tiles_n = ceil_div(p.N, 16);
     const int waves = min(FEW_WAVES, p.steps);
     const int blocks = min(p.tiles_n, 256 * FEW_WAVES / waves);
-    size_t lds = (size_t)2 * waves * MT * 1024;
+    constexpr bool WINDOWS = !MASKED || X == HELD;
+    size_t lds = (size_t)few_sums(WINDOWS, SW) * waves * 1024;
+    if (WINDOWS) lds += (size_t)waves * SW * FEW_WINDOW * 16;
     if (X != HELD) lds = max(lds, (size_t)p.M * (few_code_pitch(p.steps) + few_scale_pitch(p.steps)));
-    MBU_LAUNCH((mx4_few_kernel<X, MASKED, MT, SW>), dim3((unsigned)blocks), dim3(64 * waves), lds, s, p);
+    MBU_LAUNCH((mx4_few_kernel<X, MASKED, SW>), dim3((unsigned)blocks), dim3(64 * waves), lds, s, p);
     return check_launch(fn);
 }
 
 template <int X, bool MASKED> static int choose_few(const char *fn, const Mx4Args &p, hipStream_t s)
 {
-    const int each = ceil_div(p.steps, FEW_WAVES);                 // steps of a wave
-    if (p.M <= 16) {
-        if (each <= 1) return launch_few<X, MASKED, 1, 1>(fn, p, s);
-        if (each <= 2) return launch_few<X, MASKED, 1, 2>(fn, p, s);
-        if constexpr (X == HELD) return launch_few<X, MASKED, 1, 0>(fn, p, s);
-    }
-    if constexpr (X == HELD) {
-        if (p.M <= 32) return each <= 1 ? launch_few<X, MASKED, 2, 1>(fn, p, s) : launch_few<X, MASKED, 2, 0>(fn, p, s);
-        return each <= 1 ? launch_few<X, MASKED, 4, 1>(fn, p, s) : launch_few<X, MASKED, 4, 0>(fn, p, s);
-    }
-    return fail(MBU_ERR_SHAPE, "%s: no kernel", fn);
+    return p.steps <= FEW_WAVES ? launch_few<X, MASKED, 1>(fn, p, s) : launch_few<X, MASKED, 2>(fn, p, s);
 }
 
-// Rows of floats that a product quantises on the way: every block quantises all of them, which beyond 2^17 values takes
-// longer than a launch that quantises them once (8 x 14336 by 4096 outputs: 12.8 against 9.9 us and a launch of 2.5;
-// 16 x 16384: 18.9 against 10.5 and 3).  The fragments of all inputs have to fit into registers.
-bool mx4_few_floats(int M, int K)
-{
-    const int steps = ceil_div(mx4_padded(K), 512);
-    return M <= 16 && steps <= 2 * FEW_WAVES && M * steps <= 256;
-}
+// the fragments of all inputs have to fit into registers
+bool mx4_few_fits(int M, int K) { return M <= 16 && ceil_div(mx4_padded(K), 512) <= 2 * FEW_WAVES; }
+
+// Rows of floats that a product quantises on the way: every block quantises all of them, which beyond 2^16 values takes
+// longer than a launch that quantises them once (8 x 14336 by 4096 outputs: 12.7 us in one launch, 10.2 in two;
+// 16 x 8192 by 28672: 28.1, 26.7).  At 2^16 both take about the same (16 x 4096 by 4096: 6.4, 6.4; 8 x 8192 by 28672:
+// 25.5, 25.9), below it one launch is faster (4 x 4096 by 4096: 4.1, 6.4).
+bool mx4_few_floats(int M, int K) { return mx4_few_fits(M, K) && M * ceil_div(mx4_padded(K), 512) <= 128; }
 
 template <int X> static int choose_weights(const char *fn, const Mx4Args &p, bool masked, hipStream_t s)
 {
     return masked ? choose_few<X, true>(fn, p, s) : choose_few<X, false>(fn, p, s);
 }
 
-int launch_mx4_few_floats(const char *fn, const void *x, int x_dtype, int M, long long stride, bool masked, const void *w,
-                          const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
-                          hipStream_t s)
+int launch_mx4_few(const char *fn, const Mx4Args &p, int x_type, bool masked, hipStream_t s)
 {
-    const int kp = mx4_padded(K);
-    const Mx4Args p = {x, nullptr, w, ws, alpha, bias, out, stride, M, N, K, kp, ceil_div(kp, 512), 0, dtype};
-    if (x_dtype == MBU_FLOAT32) return choose_weights<MBU_FLOAT32>(fn, p, masked, s);
-    if (x_dtype == MBU_FLOAT16) return choose_weights<MBU_FLOAT16>(fn, p, masked, s);
+    if (x_type == HELD) return choose_weights<HELD>(fn, p, masked, s);
+    if (x_type == MBU_FLOAT32) return choose_weights<MBU_FLOAT32>(fn, p, masked, s);
+    if (x_type == MBU_FLOAT16) return choose_weights<MBU_FLOAT16>(fn, p, masked, s);
     return choose_weights<MBU_BFLOAT16>(fn, p, masked, s);
-}
-
-int launch_mx4_matmul(const char *fn, const uint8_t *a, const uint8_t *as, int M, bool masked, const void *w,
-                      const uint8_t *ws, int N, int K, const float *alpha, const float *bias, void *out, int dtype,
-                      hipStream_t s)
-{
-    const int kp = mx4_padded(K);
-    const Mx4Args p = {a, as, w, ws, alpha, bias, out, 0, M, N, K, kp, ceil_div(kp, 512), 0, dtype};
-    if (M <= 64) return choose_weights<HELD>(fn, p, masked, s);
-    return masked ? launch_mx4_tile_masked(fn, p, s) : launch_mx4_tile_held(fn, p, s);
 }
 
 }  // namespace mbu

@@ -26,6 +26,18 @@ __device__ __forceinline__ v4i load16(__amdgpu_buffer_rsrc_t rs, int lane_off, i
 {
     return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0));
 }
+// 16 bytes a lane straight into LDS, one lane's behind those of the lane before it
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rs, v4i *to, int lane_off, int off)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)to, 16, lane_off,
+                                             __builtin_amdgcn_readfirstlane(off), 0, 0);
+}
+__device__ __forceinline__ void load4_to_lds(__amdgpu_buffer_rsrc_t rs, v4i *to, int lane_off, int off)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)to, 4, lane_off,
+                                             __builtin_amdgcn_readfirstlane(off), 0, 0);
+}
+constexpr int LGKM_0 = 0xc07f, VM_0 = 0x0f70;                       // s_waitcnt lgkmcnt(0), vmcnt(0)
 __device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
 {
     return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0);
@@ -100,7 +112,10 @@ __device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT
     else store_as<MT, NT, __bf16>(p, acc, m, o);
 }
 
-// Tiled kernels for many rows (mx4_tile_held.hip, mx4_tile_masked.hip); p.x holds codes
+// At most 16 rows (mx4_few.hip): x_type HELD, or the type of rows of floats that are quantised on the way.
+int launch_mx4_few(const char *fn, const Mx4Args &p, int x_type, bool masked, hipStream_t s);
+// Few tiles (mx4_wave.hip), and many (mx4_tile_held.hip, mx4_tile_masked.hip); p.x holds codes.
+int launch_mx4_wave(const char *fn, const Mx4Args &p, bool masked, hipStream_t s);
 int launch_mx4_tile_held(const char *fn, const Mx4Args &p, hipStream_t s);
 int launch_mx4_tile_masked(const char *fn, const Mx4Args &p, hipStream_t s);
 

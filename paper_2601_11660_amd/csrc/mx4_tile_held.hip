@@ -22,11 +22,11 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
 {
     constexpr int BM = 16 * MT * MW, BN = 16 * NT * NW, THREADS = 64 * MW * NW, ROWS = BM + BN;
     constexpr int UNITS = ROWS * 8 / THREADS, UNITS_A = BM * 8 / THREADS, STRIDE = THREADS / 8;
-    constexpr int SCALES = (ROWS + THREADS - 1) / THREADS;       // rows whose scales a thread stages
+    constexpr int X_ROWS = BM > THREADS / 2 ? BM : THREADS / 2, SCALE_ROWS = X_ROWS + (BN > THREADS / 2 ? BN : THREADS / 2);
     static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0 && STRIDE % 8 == 0 && MT % 4 == 0 && NT <= 8, "");
-    static_assert(BM % 64 == 0 && THREADS % 64 == 0, "the scales of a wave's threads belong to one operand");
+    static_assert(2 * BM <= THREADS && 2 * BN <= THREADS, "a thread stages 16 scales of one row");
     __shared__ v4i window[2][ROWS * 8];
-    __shared__ v4i window_scales[2][SCALES * THREADS];           // behind ROWS: zeros, never read
+    __shared__ v4i window_scales[4][SCALE_ROWS];                 // of four steps; rows behind BM and BN: zeros, never read
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4, wn = wave % NW, wm = wave / NW;
     const TileAt at = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
@@ -34,14 +34,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
 
     const int pitch = p.kp >> 1, spitch = p.kp >> 5, steps = p.steps;
     const __amdgpu_buffer_rsrc_t xr = rows_of(p.x, m0, p.M, BM, pitch), wr = rows_of(p.w, n0, p.N, BN, pitch);
-    // scales: the rows of one operand for each wave
-    __amdgpu_buffer_rsrc_t sr[SCALES];
-#pragma unroll
-    for (int q = 0; q < SCALES; ++q) {
-        const int row = wave * 64 + q * THREADS;                 // the wave's first one
-        const bool x = row < BM;
-        sr[q] = rows_of(x ? p.xs : p.ws, x ? m0 + row : n0 + (row - BM), x ? p.M : p.N, row < ROWS ? 64 : 0, spitch);
-    }
+    const __amdgpu_buffer_rsrc_t xsr = rows_of(p.xs, m0, p.M, BM, spitch), wsr = rows_of(p.ws, n0, p.N, BN, spitch);
 
     const int srow = tid >> 3, schunk = tid & 7;                 // what the thread stages: rows srow + STRIDE q
     const int lane_off = srow * pitch + schunk * 16, write_unit = phase_unit(srow, schunk);
@@ -64,29 +57,34 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
         return q < UNITS_A ? load16(xr, off, q * STRIDE * pitch + phase * 128)
                            : load16(wr, off, (q - UNITS_A) * STRIDE * pitch + phase * 128);
     };
-    // the 16 scales of a row's step, in the order in which the lanes take them: word g of the row for lane group g
-    auto fetch_scales = [&](int q, int step) { return load16(sr[q], lane * spitch, step * 16); };
-    auto in_lane_order = [&](v4i s, int step) {
+    // Scales of two steps at a time, 32 bytes of a row by two lanes (step by step, a lane per row, they were 64 accesses a
+    // load, a fifth of all): those of the activations for steps s + 2 and s + 3 in an even step s, those of the weights in
+    // an odd one.  They are put down in the order in which the lanes take them, word g of a row for lane group g.
+    const int scale_row = tid >> 1, scale_part = tid & 1, scale_off = scale_row * spitch + scale_part * 16;
+    auto fetch_scales = [&](bool x, int step) { return load16(x ? xsr : wsr, scale_off, step * 16); };
+    auto put_scales = [&](bool x, int step, v4i s) {
+        step += scale_part;
         s = mx4_row_end(s, spitch - step * 16);
-        return (v4i){(int)mx4_scales_of(s, 0), (int)mx4_scales_of(s, 1), (int)mx4_scales_of(s, 2), (int)mx4_scales_of(s, 3)};
+        window_scales[step & 3][(x ? 0 : X_ROWS) + scale_row] =
+            (v4i){(int)mx4_scales_of(s, 0), (int)mx4_scales_of(s, 1), (int)mx4_scales_of(s, 2), (int)mx4_scales_of(s, 3)};
     };
 
-    v4i st[UNITS], ss[SCALES], f[4], wf[2][NT];
+    v4i st[UNITS], ss, f[4], wf[2][NT];
     uint32_t xs[MT], ws[NT], ws2[NT];
 #pragma unroll
     for (int q = 0; q < UNITS; ++q) st[q] = fetch(q, 0);
-#pragma unroll
-    for (int q = 0; q < SCALES; ++q) ss[q] = fetch_scales(q, 0);
+    const v4i s0 = fetch_scales(true, 0), s1 = fetch_scales(false, 0), s2 = fetch_scales(false, 1);
 #pragma unroll
     for (int q = 0; q < UNITS; ++q) {
         window[0][write_unit + q * STRIDE * 8] = st[q];
         st[q] = fetch(q, 1);
     }
-#pragma unroll
-    for (int q = 0; q < SCALES; ++q) window_scales[0][q * THREADS + tid] = in_lane_order(ss[q], 0);
+    put_scales(true, 0, s0);
+    put_scales(false, 0, s1);
+    put_scales(false, 1, s2);
     __syncthreads();
     const uint32_t *const scales = reinterpret_cast<const uint32_t *>(window_scales);
-    const int xs_at = x_row * 4 + g, ws_at = w_row * 4 + g;
+    const int xs_at = x_row * 4 + g, ws_at = (X_ROWS + w_row - BM) * 4 + g;
 #pragma unroll
     for (int n = 0; n < NT; ++n) wf[0][n] = window[0][w_unit[0] + n * 128];
 #pragma unroll
@@ -97,8 +95,9 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
     xs[1] = scales[xs_at + 64];
 
     for (int step = 0; step < steps; ++step) {
-        const uint32_t *const cur_scales = scales + (step & 1) * (SCALES * THREADS * 4);
-        const uint32_t *const nxt_scales = scales + ((step & 1) ^ 1) * (SCALES * THREADS * 4);
+        const uint32_t *const cur_scales = scales + (step & 3) * (SCALE_ROWS * 4);
+        const uint32_t *const nxt_scales = scales + ((step + 1) & 3) * (SCALE_ROWS * 4);
+        const bool even = (step & 1) == 0;
         repeat<2>([&](auto half) {
             constexpr int H = decltype(half)::value, GROUPS = 2 * MT, WHOLE = GROUPS - 4;
             const v4i *const cur = window[H];
@@ -128,15 +127,8 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
                         st[q] = fetch(q, 2 * step + H + 2);
                     }
                 });
-                if constexpr (H == 0 && G == MT) {
-#pragma unroll
-                    for (int q = 0; q < SCALES; ++q) ss[q] = fetch_scales(q, step + 1);
-                }
-                if constexpr (H == 1 && G == WHOLE - 2) {
-#pragma unroll
-                    for (int q = 0; q < SCALES; ++q)
-                        window_scales[(step & 1) ^ 1][q * THREADS + tid] = in_lane_order(ss[q], step + 1);
-                }
+                if constexpr (H == 0 && G == MT) ss = fetch_scales(even, step + 2);
+                if constexpr (H == 1 && G == WHOLE - 2) put_scales(even, step + 2, ss);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     acc[i][n] = mx4_mfma<j>(wf[G / MT][n], ws[n], f[G & 3], xs[i], acc[i][n]);
@@ -160,9 +152,12 @@ template <int MW, int NW, int MT, int NT> static int launch_held(const char *fn,
 
 int launch_mx4_tile_held(const char *fn, const Mx4Args &p, hipStream_t s)
 {
+    // large tiles where they keep three quarters of the compute units busy, small ones until every compute unit has
+    // its two blocks of the middle ones (256 x 256, 128 x 128, 64 x 128: 300 x 28672 x 8192 60.8, 61.6 and 87.5 us;
+    // 512 x 14336 x 4096 36.8, 26.3, 32.1; 512 x 4096 x 4096 33.6, 16.4, 11.8)
     if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_held<2, 4, 8, 4>(fn, p, s);
-    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_held<2, 2, 4, 4>(fn, p, s);
-    return launch_held<1, 4, 4, 1>(fn, p, s);
+    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) > 256) return launch_held<2, 2, 4, 4>(fn, p, s);
+    return launch_held<1, 4, 4, 2>(fn, p, s);
 }
 
 }  // namespace mbu

@@ -1,7 +1,7 @@
 // Products of activations in the microscaled 4-bit format with masked-binary weights, for many rows: activations through
 // LDS, weights straight into registers.
 //
-// A block takes 16 MT MW rows by 4 x 16 NT outputs, a wave 16 MT by 16 NT of them.  The sum runs in steps of 512 inputs.
+// A block of four waves takes 16 MT rows by 64 NT outputs, a wave all rows by 16 NT outputs.  The sum runs in steps of 512 inputs.
 // The activations of a step (256 bytes of a row) are shared by the waves and go through a double-buffered LDS window; the
 // weights lie in the order in which the lanes read them, two bits each, and need no window: a load of 16 bytes per lane
 // is one run of 1 KB and feeds two matrix instructions after a shift and two masks.
@@ -13,18 +13,18 @@ namespace mbu {
 // over all banks
 __device__ __forceinline__ int window_unit(int row, int chunk) { return row * 16 + (chunk ^ (row & 15)); }
 
-template <int MW, int MT, int NT>
-__global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4Args p)
+template <int MT, int NT>
+__global__ __launch_bounds__(256, 2) void mx4_tile_masked_kernel(const Mx4Args p)
 {
-    constexpr int BM = 16 * MT * MW, BN = 64 * NT, THREADS = 256 * MW;
+    constexpr int BM = 16 * MT, BN = 64 * NT;
     __shared__ v4i window[2][BM * 16];
-    __shared__ v4i window_scales[2][THREADS];                    // rows behind BM: zeros, never read
+    __shared__ v4i window_scales[2][256];                        // rows behind BM: zeros, never read
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r = lane & 15, g = lane >> 4, wn = wave & 3, wm = wave >> 2;
+    const int r = lane & 15, g = lane >> 4;
 
     const TileAt at_tile = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
     const int tm = at_tile.m, tn = at_tile.n;
-    const uint32_t m0 = (uint32_t)tm * BM, n0 = (uint32_t)tn * BN + wn * 16 * NT;
+    const uint32_t m0 = (uint32_t)tm * BM, n0 = (uint32_t)tn * BN + wave * 16 * NT;
 
     const int pitch = p.kp >> 1, spitch = p.kp >> 5, steps = p.steps;
     const __amdgpu_buffer_rsrc_t xr = rows_of(p.x, m0, p.M, BM, pitch), xsr = rows_of(p.xs, m0, p.M, BM, spitch);
@@ -32,13 +32,12 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4A
     const uint32_t tiles_w = ((uint32_t)p.N + 15) / 16;
     const __amdgpu_buffer_rsrc_t wr = rows_of(p.w, nw / 16, tiles_w, NT, steps * 2048);
 
-    const int srow = tid >> 4, schunk = tid & 15;                // what the thread stages: rows srow + 16 MW q
+    const int srow = tid >> 4, schunk = tid & 15;                // what the thread stages: rows srow + 16 q
     const int x_lane = srow * pitch + schunk * 16, xs_lane = tid < BM ? tid * spitch : OUT_OF_RANGE;
     const int write_unit = window_unit(srow, schunk);
-    const int read_row = wm * 16 * MT + r;
     int read_unit[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) read_unit[j] = window_unit(read_row, 4 * j + g);
+    for (int j = 0; j < 4; ++j) read_unit[j] = window_unit(r, 4 * j + g);
 
     v4f acc[MT][NT];
 #pragma unroll
@@ -59,7 +58,7 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4A
     constexpr uint32_t ONE = 0x7f7f7f7fu;                        // scales 2^0
     auto stage = [&](int q, int step) {
         const int off = step * 256 + schunk * 16 < pitch ? x_lane : OUT_OF_RANGE;
-        return load16(xr, off, q * 16 * MW * pitch + step * 256);
+        return load16(xr, off, q * 16 * pitch + step * 256);
     };
     // the scales of one row, in the order in which the lanes take them: word g of a row for lane group g
     auto stage_scales = [&](int step) { return load16(xsr, xs_lane, step * 16); };
@@ -76,14 +75,14 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4A
         load_weights(0, 0);
         load_weights(1, 0);
 #pragma unroll
-        for (int q = 0; q < MT; ++q) window[0][write_unit + q * 256 * MW] = st[q];
+        for (int q = 0; q < MT; ++q) window[0][write_unit + q * 256] = st[q];
         window_scales[0][tid] = in_lane_order(ss, 0);
     }
     __syncthreads();
 
     for (int step = 0; step < steps; ++step) {
         const v4i *cur = window[step & 1];
-        const uint32_t *cur_scales = reinterpret_cast<const uint32_t *>(window_scales[step & 1]) + read_row * 4 + g;
+        const uint32_t *cur_scales = reinterpret_cast<const uint32_t *>(window_scales[step & 1]) + r * 4 + g;
         v4i *nxt = window[(step & 1) ^ 1];
         uint32_t xs[MT];
         v4i st[MT], f[4], ss;
@@ -101,7 +100,7 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4A
             if constexpr (G % EVERY == 0 && G / EVERY < MT) st[G / EVERY] = stage(G / EVERY, step + 1);
             if constexpr (G == MT) ss = stage_scales(step + 1);
             if constexpr (G >= BEHIND && (G - BEHIND) % EVERY == 0 && (G - BEHIND) / EVERY < MT)
-                nxt[write_unit + (G - BEHIND) / EVERY * 256 * MW] = st[(G - BEHIND) / EVERY];
+                nxt[write_unit + (G - BEHIND) / EVERY * 256] = st[(G - BEHIND) / EVERY];
             if constexpr (G == GROUPS - 1) window_scales[(step & 1) ^ 1][tid] = in_lane_order(ss, step + 1);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -112,23 +111,24 @@ __global__ __launch_bounds__(256 * MW, 2) void mx4_tile_masked_kernel(const Mx4A
         __syncthreads();
     }
 
-    store_tile<MT, NT>(p, acc, m0 + wm * 16 * MT + r, n0 + 4 * g);
+    store_tile<MT, NT>(p, acc, m0 + r, n0 + 4 * g);
 }
 
-template <int MW, int MT, int NT> static int launch_masked(const char *fn, Mx4Args p, hipStream_t s)
+template <int MT, int NT> static int launch_masked(const char *fn, Mx4Args p, hipStream_t s)
 {
     p.tiles_n = ceil_div(p.N, 64 * NT);
-    const long long blocks = (long long)ceil_div(p.M, 16 * MT * MW) * p.tiles_n;
+    const long long blocks = (long long)ceil_div(p.M, 16 * MT) * p.tiles_n;
     if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "%s: product too large", fn);
-    MBU_LAUNCH((mx4_tile_masked_kernel<MW, MT, NT>), dim3((unsigned)blocks), dim3(256 * MW), 0, s, p);
+    MBU_LAUNCH((mx4_tile_masked_kernel<MT, NT>), dim3((unsigned)blocks), dim3(256), 0, s, p);
     return check_launch(fn);
 }
 
 int launch_mx4_tile_masked(const char *fn, const Mx4Args &p, hipStream_t s)
 {
-    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_masked<2, 8, 4>(fn, p, s);
-    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) >= 192) return launch_masked<1, 8, 2>(fn, p, s);
-    return launch_masked<1, 4, 1>(fn, p, s);
+    // large tiles where every compute unit has its two blocks of them (128 x 256 against 64 x 128: 2048 x 8192 x 8192
+    // 64.8 and 77.0 us, 300 x 28672 x 8192 54.1 and 47.9, 1024 x 4096 x 4096 24.2 and 13.4)
+    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 256) >= 512) return launch_masked<8, 4>(fn, p, s);
+    return launch_masked<4, 2>(fn, p, s);
 }
 
 }  // namespace mbu

@@ -1,0 +1,169 @@
+// Products in the microscaled 4-bit format for a moderate number of rows: the waves of a block split the inputs.
+//
+// With tiles this small the time is neither the matrix instructions nor the memory but what lies between them: the
+// address unit takes a cycle for every 64 bytes that neighbouring lanes do not share, LDS has to carry an operand once for
+// every wave that wants it, and barriers line all of it up.  So each of a block's eight waves takes the whole tile, 16 MT
+// rows by 16 NT outputs, for a share of the inputs of its own: it fetches 128 consecutive bytes of a row with eight
+// lanes, turns them round in an LDS window that is its own (a lane of the matrix instruction holds a row), and waits for
+// nobody.  The sums are added up in LDS at the end, in the waves' order.  (Tiles of 64 x 64 whose four waves share
+// operands and barriers took 0.76 us for 512 inputs; 200 x 4096 x 14336 25.4 us.)
+#include "mx4_product.h"
+
+namespace mbu {
+
+constexpr int WAVES = 8;
+
+// unit of 16 bytes `chunk` (of eight) of a row of a window: eight rows at one chunk lie in different banks
+__device__ __forceinline__ int wave_unit(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
+
+template <bool MASKED, int MT, int NT>
+__global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p)
+{
+    constexpr int BM = 16 * MT, BN = 16 * NT, ROWS = MASKED ? BM : BM + BN, XU = BM / 8, UNITS = ROWS / 8;
+    constexpr int SU = (ROWS + 31) / 32;                             // fetches of scales: four turns of 32 rows
+    __shared__ v4i windows[WAVES][ROWS * 8 > MT * NT * 64 ? ROWS * 8 : MT * NT * 64];
+    __shared__ v4i window_scales[WAVES][SU * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const TileAt at = tile_of_block(p.tiles_n, (int)(((uint32_t)p.M + BM - 1) / BM));
+    const uint32_t m0 = (uint32_t)at.m * BM, n0 = (uint32_t)at.n * BN;
+    v4i *const window = windows[wave], *const scales = window_scales[wave];
+
+    // the wave's turns of 256 inputs
+    const int pitch = p.kp >> 1, spitch = p.kp >> 5, turns = (p.kp + 255) >> 8, share = (turns + WAVES - 1) / WAVES;
+    const int begin = min(wave * share, turns), end = min(begin + share, turns);
+    const __amdgpu_buffer_rsrc_t xr = rows_of(p.x, m0, p.M, BM, pitch), xsr = rows_of(p.xs, m0, p.M, BM, spitch);
+    const __amdgpu_buffer_rsrc_t wr = MASKED ? rows_of(p.w, n0 / 16, ((uint32_t)p.N + 15) / 16, NT, p.steps * 2048)
+                                             : rows_of(p.w, n0, p.N, BN, pitch);
+    const __amdgpu_buffer_rsrc_t wsr = rows_of(MASKED ? p.xs : p.ws, MASKED ? 0 : n0, MASKED ? 0 : p.N, BN, spitch);
+    const int chunk = (lane & 7) ^ (lane >> 3), row_off = (lane >> 3) * pitch + chunk * 16;
+    const int scale_off = (lane >> 1) * spitch + (lane & 1) * 16;
+    const int read[2] = {wave_unit(r, g), wave_unit(r, 4 + g)};
+
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = (v4f){0, 0, 0, 0};
+    v4i ss[SU], wm[NT];
+
+    // straight into the window: a lane's 16 bytes go behind those of the lane before it, eight lanes to a row, so that
+    // the order of the chunks in a row is that of the addresses
+    auto fetch = [&](int turn) {
+        const int off = turn < end && turn * 128 + chunk * 16 < pitch ? row_off : OUT_OF_RANGE;
+#pragma unroll
+        for (int q = 0; q < UNITS; ++q)
+            if (q < XU) load_to_lds(xr, window + q * 64, off, q * 8 * pitch + turn * 128);
+            else load_to_lds(wr, window + q * 64, off, (q - XU) * 8 * pitch + turn * 128);
+        if (MASKED) {
+            const int at = turn < end ? lane * 16 : OUT_OF_RANGE;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) wm[n] = load16(wr, at, n * p.steps * 2048 + turn * 1024);
+        }
+    };
+    // the scales of four turns: 32 bytes of a row
+    auto fetch_scales = [&](int turn) {
+        const int off = turn < end ? scale_off : OUT_OF_RANGE;
+#pragma unroll
+        for (int q = 0; q < SU; ++q)
+            ss[q] = q < BM / 32 ? load16(xsr, off, q * 32 * spitch + turn * 8)
+                                : load16(wsr, off, (q - BM / 32) * 32 * spitch + turn * 8);
+    };
+
+    fetch_scales(begin);
+    fetch(begin);
+    for (int turn = begin; turn < end; ++turn) {
+        const int part = (turn - begin) & 3;
+        // what was fetched into the window is there
+        __builtin_amdgcn_s_waitcnt(VM_0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (part == 0) {
+#pragma unroll
+            for (int q = 0; q < SU; ++q) scales[q * 64 + lane] = ss[q];
+        }
+        // bytes g and 4 + g of a row's eight; behind the row's end lie another row's
+        const uint2 *const sc = reinterpret_cast<const uint2 *>(scales) + part;
+        const uint32_t pick = 0x0c0c0400u + 0x0101u * (uint32_t)g, second = turn * 8 + 4 < spitch ? ~0u : 0u;
+        uint32_t xs[MT], ws[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const uint2 s = sc[(16 * i + r) * 4];
+            xs[i] = __builtin_amdgcn_perm(s.y & second, s.x, pick);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            ws[n] = 0x7f7f7f7fu;
+            if (!MASKED) {
+                const uint2 s = sc[(BM + 16 * n + r) * 4];
+                ws[n] = __builtin_amdgcn_perm(s.y & second, s.x, pick);
+            }
+        }
+        v4i x[2][MT], w[2][NT];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x[j][i] = window[read[j] + i * 128];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                w[j][n] = !MASKED ? window[read[j] + (MT + n) * 128]
+                          : j     ? expand_masked((uint32_t)wm[n].z, (uint32_t)wm[n].w)
+                                  : expand_masked((uint32_t)wm[n].x, (uint32_t)wm[n].y);
+        }
+        // the next turn goes into the same window, as soon as this one's operands are out of it
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(LGKM_0);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(turn + 1);
+        if (part == 0) fetch_scales(turn + 4);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[i][n] = mx4_mfma<0>(w[0][n], ws[n], x[0][i], xs[i], acc[i][n]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[i][n] = mx4_mfma<1>(w[1][n], ws[n], x[1][i], xs[i], acc[i][n]);
+    }
+
+    // every wave adds up some of the fragments
+    v4f *const part = reinterpret_cast<v4f *>(windows[0]);
+    constexpr int APART = sizeof(windows[0]) / 16;
+#pragma unroll
+    for (int f = 0; f < MT * NT; ++f) part[wave * APART + f * 64 + lane] = acc[f / NT][f % NT];
+    __syncthreads();
+    const int used = (turns + share - 1) / share;
+#pragma unroll
+    for (int k = 0; k < (MT * NT + WAVES - 1) / WAVES; ++k) {
+        const int f = k * WAVES + wave;
+        if (f >= MT * NT) continue;
+        v4f v[1][1] = {{part[f * 64 + lane]}};
+        for (int s = 1; s < used; ++s) v[0][0] += part[s * APART + f * 64 + lane];
+        store_tile<1, 1>(p, v, m0 + f / NT * 16 + r, n0 + f % NT * 16 + 4 * g);
+    }
+}
+
+template <bool MASKED, int MT, int NT> static int launch_wave(const char *fn, Mx4Args p, hipStream_t s)
+{
+    p.tiles_n = ceil_div(p.N, 16 * NT);
+    const long long blocks = (long long)ceil_div(p.M, 16 * MT) * p.tiles_n;
+    if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "%s: product too large", fn);
+    MBU_LAUNCH((mx4_wave_kernel<MASKED, MT, NT>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, p);
+    return check_launch(fn);
+}
+
+template <bool MASKED> static int choose_wave(const char *fn, const Mx4Args &p, hipStream_t s)
+{
+    // the smallest tile that leaves no compute unit with two (64 rows by 4096 x 4096 in tiles of 32 x 32, 32 x 64 and
+    // 64 x 64: 5.1, 6.4 and 8.8 us; 100 rows: 7.1, 6.6, 8.8; 200 by 14336 inputs: 27, 25.6, 18.4)
+    if ((long long)ceil_div(p.M, 32) * ceil_div(p.N, 32) <= 256) return launch_wave<MASKED, 2, 2>(fn, p, s);
+    if ((long long)ceil_div(p.M, 32) * ceil_div(p.N, 64) <= 256) return launch_wave<MASKED, 2, 4>(fn, p, s);
+    return launch_wave<MASKED, 4, 4>(fn, p, s);
+}
+
+int launch_mx4_wave(const char *fn, const Mx4Args &p, bool masked, hipStream_t s)
+{
+    return masked ? choose_wave<true>(fn, p, s) : choose_wave<false>(fn, p, s);
+}
+
+}  // namespace mbu

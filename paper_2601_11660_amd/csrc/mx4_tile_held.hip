@@ -7,7 +7,7 @@
 //
 // A block takes 16 MT MW rows by 16 NT NW outputs, a wave 16 MT by 16 NT of them.  Phases of 256 inputs (128 bytes of a row)
 // go through two windows.  In phase t a wave multiplies out of one window; in its first half it writes phase t + 1, which
-// it fetched a phase ago, into the other one, and fetches phase t + 2; a barrier in the middle of the phase makes that
+// it fetched a phase ago, into the other one, and fetches phase t + 2; a barrier in the third quarter makes that
 // window whole, so that the first operands of phase t + 1 are read before phase t ends and no wave waits for them.  The
 // barrier at the start of a phase stands before the writes: by then every wave has multiplied what it read there.
 #include "mx4_product.h"
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
         const uint32_t *const nxt_scales = scales + ((step + 1) & 3) * (SCALE_ROWS * 4);
         const bool even = (step & 1) == 0;
         repeat<2>([&](auto half) {
-            constexpr int H = decltype(half)::value, GROUPS = 2 * MT, WHOLE = GROUPS - 4;
+            constexpr int H = decltype(half)::value, GROUPS = 2 * MT, WHOLE = GROUPS - 4, SPAN = MT > 4 ? WHOLE - 4 : WHOLE;
             const v4i *const cur = window[H];
             v4i *const nxt = window[H ^ 1];
             __builtin_amdgcn_s_barrier();
@@ -107,7 +107,11 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
             repeat<GROUPS>([&](auto group) {
                 constexpr int G = decltype(group)::value, i = G % MT, j = 2 * H + G / MT;
                 if constexpr (G == WHOLE) {
-                    __syncthreads();
+                    // LDS answers in order: the writes are done, only the reads of the groups since may be on their way
+                    __builtin_amdgcn_s_waitcnt(LGKM_0 | (WHOLE - SPAN) << 8);
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if constexpr (G + 3 < GROUPS) f[(G + 3) & 3] = cur[x_unit[(G + 3) / MT] + (G + 3) % MT * 128];
@@ -122,13 +126,13 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
                 if constexpr (H == 1 && G >= GROUPS - 2) xs[G - (GROUPS - 2)] = nxt_scales[xs_at + (G - (GROUPS - 2)) * 64];
                 repeat<UNITS>([&](auto unit) {
                     constexpr int q = decltype(unit)::value;
-                    if constexpr (G == q * WHOLE / UNITS) {
+                    if constexpr (G == q * SPAN / UNITS) {
                         nxt[write_unit + q * STRIDE * 8] = st[q];
                         st[q] = fetch(q, 2 * step + H + 2);
                     }
                 });
                 if constexpr (H == 0 && G == MT) ss = fetch_scales(even, step + 2);
-                if constexpr (H == 1 && G == WHOLE - 2) put_scales(even, step + 2, ss);
+                if constexpr (H == 1 && G == 2) put_scales(even, step + 2, ss);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     acc[i][n] = mx4_mfma<j>(wf[G / MT][n], ws[n], f[G & 3], xs[i], acc[i][n]);

@@ -190,6 +190,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
     }
     for (int turn = 0; tile < tiles; ++turn) {
         const int next = tile + gridDim.x;
+        const bool adds = turn % waves == wave;                    // the waves take turns at adding up
+        Mx4Ends<1> ends;
+        if (adds) ends.load(p, (uint32_t)tile * 16 + 4 * g);
         v4f acc = {0, 0, 0, 0};
         auto multiply = [&](int k, int step) {
             const uint32_t s = w[k].scales(p, step, g);
@@ -219,12 +222,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
                     fetch_rows(window + k * FEW_WINDOW, p.w, p.ws, (uint32_t)next * 16, p.N, pitch, spitch, wave + k * waves, lane);
             }
         __syncthreads();
-        // the waves take turns at adding up
-        if (turn % waves == wave) {
+        if (adds) {
             const v4f *const sums = part + (turn % SUMS) * waves * 64 + lane;
             v4f v[1][1] = {{sums[0]}};
             for (int s = 1; s < waves; ++s) v[0][0] += sums[s * 64];
-            store_tile<1, 1>(p, v, r, (uint32_t)tile * 16 + 4 * g);
+            store_tile<1, 1>(p, v, ends, r, (uint32_t)tile * 16 + 4 * g);
         }
         if (SUMS == 1) __syncthreads();
         tile = next;

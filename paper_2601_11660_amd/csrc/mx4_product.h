@@ -74,26 +74,37 @@ __device__ __forceinline__ TileAt tile_of_block(int tiles_n, int tiles_m)
     return {band * 4 + in % high, in / high};
 }
 
+// Factor and bias of outputs o + 16 n + 0..3; zeros behind the last one.  They are asked for together and ahead of their
+// use: one after another, each in front of its stores, they were NT waits for memory at the end of every tile.
+template <int NT> struct Mx4Ends {
+    v4f alpha[NT], bias[NT];
+    __device__ __forceinline__ void load(const Mx4Args &p, uint32_t o)
+    {
+        const uint32_t first = __builtin_amdgcn_readfirstlane(o);
+        const __amdgpu_buffer_rsrc_t ar = rows_of(p.alpha, first, p.alpha ? p.N : 0, 16 * NT, 4);
+        const __amdgpu_buffer_rsrc_t br = rows_of(p.bias, first, p.bias ? p.N : 0, 16 * NT, 4);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            alpha[n] = __builtin_bit_cast(v4f, load16(ar, (int)(o - first) * 4, n * 64));
+            bias[n] = __builtin_bit_cast(v4f, load16(br, (int)(o - first) * 4, n * 64));
+        }
+    }
+};
+
 template <int MT, int NT, typename OT>
-__device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+__device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
+                                         uint32_t o)
 {
 #pragma unroll
     for (int n = 0; n < NT; ++n, o += 16) {
         if (o >= (uint32_t)p.N) continue;
         const int left = (int)min(4u, (uint32_t)p.N - o);
-        v4f alpha = {1, 1, 1, 1}, bias = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < left) {
-                if (p.alpha) alpha[q] = p.alpha[o + q];
-                if (p.bias) bias[q] = p.bias[o + q];
-            }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             if (m + 16 * i >= (uint32_t)p.M) continue;
             v4f v = acc[i][n];
-            if (p.alpha) v *= alpha;
-            if (p.bias) v += bias;
+            if (p.alpha) v *= ends.alpha[n];
+            if (p.bias) v += ends.bias[n];
             OT *dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + o;
             if ((p.N & 3) == 0) mx4_store4(dst, v);
             else
@@ -105,11 +116,19 @@ __device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][
 }
 // Factor, bias, the one rounding, and the stores of a wave: acc[i][n] holds outputs o + 16 n + 0..3 of row m + 16 i.
 template <int MT, int NT>
+__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
+                                           uint32_t o)
+{
+    if (p.dtype == MBU_FLOAT32) store_as<MT, NT, float>(p, acc, ends, m, o);
+    else if (p.dtype == MBU_FLOAT16) store_as<MT, NT, _Float16>(p, acc, ends, m, o);
+    else store_as<MT, NT, __bf16>(p, acc, ends, m, o);
+}
+template <int MT, int NT>
 __device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
 {
-    if (p.dtype == MBU_FLOAT32) store_as<MT, NT, float>(p, acc, m, o);
-    else if (p.dtype == MBU_FLOAT16) store_as<MT, NT, _Float16>(p, acc, m, o);
-    else store_as<MT, NT, __bf16>(p, acc, m, o);
+    Mx4Ends<NT> ends;
+    ends.load(p, o);
+    store_tile<MT, NT>(p, acc, ends, m, o);
 }
 
 // At most 16 rows (mx4_few.hip): x_type HELD, or the type of rows of floats that are quantised on the way.

@@ -25,7 +25,8 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
     constexpr int X_ROWS = BM > THREADS / 2 ? BM : THREADS / 2, SCALE_ROWS = X_ROWS + (BN > THREADS / 2 ? BN : THREADS / 2);
     static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0 && STRIDE % 8 == 0 && MT % 4 == 0 && NT <= 8, "");
     static_assert(2 * BM <= THREADS && 2 * BN <= THREADS, "a thread stages 16 scales of one row");
-    __shared__ v4i window[2][ROWS * 8];
+    // the two windows of an operand within reach of one address and a constant (64 KB): registers are short
+    __shared__ v4i x_window[2][BM * 8], w_window[2][BN * 8];
     __shared__ v4i window_scales[4][SCALE_ROWS];                 // of four steps; rows behind BM and BN: zeros, never read
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4, wn = wave % NW, wm = wave / NW;
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
 
     const int srow = tid >> 3, schunk = tid & 7;                 // what the thread stages: rows srow + STRIDE q
     const int lane_off = srow * pitch + schunk * 16, write_unit = phase_unit(srow, schunk);
-    const int x_row = wm * 16 * MT + r, w_row = BM + wn * 16 * NT + r;
+    const int x_row = wm * 16 * MT + r, w_row = wn * 16 * NT + r;
     int x_unit[4], w_unit[4];                                    // by instruction of a step: chunk 4 (j & 1) + g
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -56,6 +57,10 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
         const int off = phase * 128 + schunk * 16 < pitch ? lane_off : OUT_OF_RANGE;
         return q < UNITS_A ? load16(xr, off, q * STRIDE * pitch + phase * 128)
                            : load16(wr, off, (q - UNITS_A) * STRIDE * pitch + phase * 128);
+    };
+    auto put = [&](int into, int q, v4i v) {
+        if (q < UNITS_A) x_window[into][write_unit + q * STRIDE * 8] = v;
+        else w_window[into][write_unit + (q - UNITS_A) * STRIDE * 8] = v;
     };
     // Scales of two steps at a time, 32 bytes of a row by two lanes (step by step, a lane per row, they were 64 accesses a
     // load, a fifth of all): those of the activations for steps s + 2 and s + 3 in an even step s, those of the weights in
@@ -76,7 +81,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
     const v4i s0 = fetch_scales(true, 0), s1 = fetch_scales(false, 0), s2 = fetch_scales(false, 1);
 #pragma unroll
     for (int q = 0; q < UNITS; ++q) {
-        window[0][write_unit + q * STRIDE * 8] = st[q];
+        put(0, q, st[q]);
         st[q] = fetch(q, 1);
     }
     put_scales(true, 0, s0);
@@ -84,13 +89,13 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
     put_scales(false, 1, s2);
     __syncthreads();
     const uint32_t *const scales = reinterpret_cast<const uint32_t *>(window_scales);
-    const int xs_at = x_row * 4 + g, ws_at = (X_ROWS + w_row - BM) * 4 + g;
+    const int xs_at = x_row * 4 + g, ws_at = (X_ROWS + w_row) * 4 + g;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) wf[0][n] = window[0][w_unit[0] + n * 128];
+    for (int n = 0; n < NT; ++n) wf[0][n] = w_window[0][w_unit[0] + n * 128];
 #pragma unroll
     for (int n = 0; n < NT; ++n) ws[n] = scales[ws_at + n * 64];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) f[i] = window[0][x_unit[0] + i * 128];
+    for (int i = 0; i < 3; ++i) f[i] = x_window[0][x_unit[0] + i * 128];
     xs[0] = scales[xs_at];
     xs[1] = scales[xs_at + 64];
 
@@ -100,8 +105,6 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
         const bool even = (step & 1) == 0;
         repeat<2>([&](auto half) {
             constexpr int H = decltype(half)::value, GROUPS = 2 * MT, WHOLE = GROUPS - 4, SPAN = MT > 4 ? WHOLE - 4 : WHOLE;
-            const v4i *const cur = window[H];
-            v4i *const nxt = window[H ^ 1];
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             repeat<GROUPS>([&](auto group) {
@@ -114,12 +117,12 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
                     asm volatile("" ::: "memory");
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (G + 3 < GROUPS) f[(G + 3) & 3] = cur[x_unit[(G + 3) / MT] + (G + 3) % MT * 128];
-                else f[(G + 3) & 3] = nxt[x_unit[0] + (G + 3 - GROUPS) * 128];
+                if constexpr (G + 3 < GROUPS) f[(G + 3) & 3] = x_window[H][x_unit[(G + 3) / MT] + (G + 3) % MT * 128];
+                else f[(G + 3) & 3] = x_window[H ^ 1][x_unit[0] + (G + 3 - GROUPS) * 128];
                 repeat<NT>([&](auto output) {
                     constexpr int n = decltype(output)::value;
-                    if constexpr (G == n * 4 / (NT > 4 ? NT : 4)) wf[1][n] = cur[w_unit[1] + n * 128];
-                    if constexpr (G == WHOLE + n * 4 / (NT > 4 ? NT : 4)) wf[0][n] = nxt[w_unit[0] + n * 128];
+                    if constexpr (G == n * 4 / (NT > 4 ? NT : 4)) wf[1][n] = w_window[H][w_unit[1] + n * 128];
+                    if constexpr (G == WHOLE + n * 4 / (NT > 4 ? NT : 4)) wf[0][n] = w_window[H ^ 1][w_unit[0] + n * 128];
                     if constexpr (H == 1 && G == WHOLE + n * 4 / (NT > 4 ? NT : 4)) ws2[n] = nxt_scales[ws_at + n * 64];
                 });
                 if constexpr (H == 0 && G + 2 < MT) xs[G + 2] = cur_scales[xs_at + (G + 2) * 64];
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
                 repeat<UNITS>([&](auto unit) {
                     constexpr int q = decltype(unit)::value;
                     if constexpr (G == q * SPAN / UNITS) {
-                        nxt[write_unit + q * STRIDE * 8] = st[q];
+                        put(H ^ 1, q, st[q]);
                         st[q] = fetch(q, 2 * step + H + 2);
                     }
                 });
@@ -142,7 +145,9 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
 #pragma unroll
         for (int n = 0; n < NT; ++n) ws[n] = ws2[n];
     }
-    store_tile<MT, NT>(p, acc, m0 + x_row, n0 + wn * 16 * NT + 4 * g);
+    int thread = tid;
+    asm volatile("" : "+v"(thread));                             // nothing of the end in front of the loop: registers are short
+    store_tile<MT, NT>(p, acc, m0 + wm * 16 * MT + (thread & 15), n0 + wn * 16 * NT + 4 * (thread >> 4 & 3));
 }
 
 template <int MW, int NW, int MT, int NT> static int launch_held(const char *fn, Mx4Args p, hipStream_t s)

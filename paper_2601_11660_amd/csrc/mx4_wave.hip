@@ -131,15 +131,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p
     constexpr int APART = sizeof(windows[0]) / 16;
 #pragma unroll
     for (int f = 0; f < MT * NT; ++f) part[wave * APART + f * 64 + lane] = acc[f / NT][f % NT];
+    constexpr int MINE = (MT * NT + WAVES - 1) / WAVES;
+    Mx4Ends<1> ends[MINE];
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) ends[k].load(p, n0 + (k * WAVES + wave) % NT * 16 + 4 * g);
     __syncthreads();
     const int used = (turns + share - 1) / share;
 #pragma unroll
-    for (int k = 0; k < (MT * NT + WAVES - 1) / WAVES; ++k) {
+    for (int k = 0; k < MINE; ++k) {
         const int f = k * WAVES + wave;
         if (f >= MT * NT) continue;
         v4f v[1][1] = {{part[f * 64 + lane]}};
         for (int s = 1; s < used; ++s) v[0][0] += part[s * APART + f * 64 + lane];
-        store_tile<1, 1>(p, v, m0 + f / NT * 16 + r, n0 + f % NT * 16 + 4 * g);
+        store_tile<1, 1>(p, v, ends[k], m0 + f / NT * 16 + r, n0 + f % NT * 16 + 4 * g);
     }
 }
 

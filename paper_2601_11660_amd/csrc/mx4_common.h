@@ -193,16 +193,14 @@ template <> struct Mx4Type<MBU_BFLOAT16> { using T = __bf16; };
 __device__ __forceinline__ void mx4_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void mx4_store(__bf16 *p, float v) { *p = (__bf16)v; }
 __device__ __forceinline__ void mx4_store(_Float16 *p, float v) { *p = (_Float16)v; }
+// four values of 2 bytes
+typedef int v2i __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ v2i mx4_pack4(v4f v)
+{
+    typedef T v4t __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(v2i, (v4t){(T)v.x, (T)v.y, (T)v.z, (T)v.w});
+}
 __device__ __forceinline__ void mx4_store4(float *p, v4f v) { *reinterpret_cast<v4f *>(p) = v; }
-__device__ __forceinline__ void mx4_store4(__bf16 *p, v4f v)
-{
-    typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<v4bf *>(p) = (v4bf){(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
-}
-__device__ __forceinline__ void mx4_store4(_Float16 *p, v4f v)
-{
-    typedef _Float16 v4h __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<v4h *>(p) = (v4h){(_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
-}
+template <typename T> __device__ __forceinline__ void mx4_store4(T *p, v4f v) { *reinterpret_cast<v2i *>(p) = mx4_pack4<T>(v); }
 
 }  // namespace mbu

@@ -87,14 +87,49 @@ template <int NT> struct Mx4Ends {
         for (int n = 0; n < NT; ++n) {
             alpha[n] = __builtin_bit_cast(v4f, load16(ar, (int)(o - first) * 4, n * 64));
             bias[n] = __builtin_bit_cast(v4f, load16(br, (int)(o - first) * 4, n * 64));
+            // without one: what changes no value, a zero's sign included
+            if (!p.alpha) alpha[n] = (v4f){1, 1, 1, 1};
+            if (!p.bias) bias[n] = (v4f){-0.f, -0.f, -0.f, -0.f};
         }
     }
+    __device__ __forceinline__ v4f apply(int n, v4f v) const { return v * alpha[n] + bias[n]; }
 };
+
+// Of four values a lane in two times sixteen outputs (a: 4 g + 0..3, b: 16 + 4 g + 0..3), eight in a row: 8 g + 0..7.
+__device__ __forceinline__ v4i eight_in_a_row(v2i a, v2i b)
+{
+    v4i v;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+        const auto halves = __builtin_amdgcn_permlane32_swap(a[d], b[d], false, false);    // of g: a0 a1 b0 b1, a2 a3 b2 b3
+        const auto both = __builtin_amdgcn_permlane16_swap(halves[0], halves[1], false, false);    // a0 a2 b0 b2, a1 a3 b1 b3
+        v[d] = (int)both[0];
+        v[2 + d] = (int)both[1];
+    }
+    return v;
+}
 
 template <int MT, int NT, typename OT>
 __device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
                                          uint32_t o)
 {
+    if constexpr (sizeof(OT) == 2 && NT % 2 == 0)
+        if ((p.N & 7) == 0) {
+            // 64 consecutive bytes of a row by four lanes instead of 32
+            const uint32_t first = __builtin_amdgcn_readfirstlane(o), at = first + 2 * (o - first);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (m + 16 * i >= (uint32_t)p.M) continue;           // all four lanes of a row or none
+                OT *const dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + at;
+#pragma unroll
+                for (int n = 0; n < NT; n += 2) {
+                    const v4i v = eight_in_a_row(mx4_pack4<OT>(ends.apply(n, acc[i][n])),
+                                                 mx4_pack4<OT>(ends.apply(n + 1, acc[i][n + 1])));
+                    if (at + 16 * n < (uint32_t)p.N) *reinterpret_cast<v4i *>(dst + 16 * n) = v;
+                }
+            }
+            return;
+        }
 #pragma unroll
     for (int n = 0; n < NT; ++n, o += 16) {
         if (o >= (uint32_t)p.N) continue;
@@ -102,9 +137,7 @@ __device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             if (m + 16 * i >= (uint32_t)p.M) continue;
-            v4f v = acc[i][n];
-            if (p.alpha) v *= ends.alpha[n];
-            if (p.bias) v += ends.bias[n];
+            const v4f v = ends.apply(n, acc[i][n]);
             OT *dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + o;
             if ((p.N & 3) == 0) mx4_store4(dst, v);
             else

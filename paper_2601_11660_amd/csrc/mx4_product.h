@@ -113,19 +113,43 @@ template <int MT, int NT, typename OT>
 __device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
                                          uint32_t o)
 {
-    if constexpr (sizeof(OT) == 2 && NT % 2 == 0)
-        if ((p.N & 7) == 0) {
-            // 64 consecutive bytes of a row by four lanes instead of 32
-            const uint32_t first = __builtin_amdgcn_readfirstlane(o), at = first + 2 * (o - first);
+    constexpr int WIDE = 16 / (int)sizeof(OT), RUN = 4 * WIDE, RUNS = 16 * NT / RUN;
+    if constexpr (RUNS >= 1)
+        if (p.N % WIDE == 0) {
+            // Runs of 64 bytes of a row by four lanes, and where there are two of them 128 by eight, an even row and the
+            // odd one behind it in turn: the even row's lanes give their second run for the odd row's first.
+            const uint32_t first = __builtin_amdgcn_readfirstlane(o), at = first + (o - first) / 4 * WIDE, odd = m & 1;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                if (m + 16 * i >= (uint32_t)p.M) continue;           // all four lanes of a row or none
-                OT *const dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + at;
+                v4i v[RUNS];
 #pragma unroll
-                for (int n = 0; n < NT; n += 2) {
-                    const v4i v = eight_in_a_row(mx4_pack4<OT>(ends.apply(n, acc[i][n])),
-                                                 mx4_pack4<OT>(ends.apply(n + 1, acc[i][n + 1])));
-                    if (at + 16 * n < (uint32_t)p.N) *reinterpret_cast<v4i *>(dst + 16 * n) = v;
+                for (int c = 0; c < RUNS; ++c)
+                    if constexpr (sizeof(OT) == 2)
+                        v[c] = eight_in_a_row(mx4_pack4<OT>(ends.apply(2 * c, acc[i][2 * c])),
+                                              mx4_pack4<OT>(ends.apply(2 * c + 1, acc[i][2 * c + 1])));
+                    else
+                        v[c] = __builtin_bit_cast(v4i, ends.apply(c, acc[i][c]));
+                const uint32_t row = m + 16 * i;
+                if constexpr (RUNS == 1) {
+                    if (row < (uint32_t)p.M && at < (uint32_t)p.N)
+                        *reinterpret_cast<v4i *>((OT *)p.out + (uint64_t)row * (uint32_t)p.N + at) = v[0];
+                } else {
+                    static_assert(RUNS % 2 == 0, "");
+                    OT *const dst = (OT *)p.out + (uint64_t)(row - odd) * (uint32_t)p.N + at + odd * RUN;
+#pragma unroll
+                    for (int c = 0; c < RUNS; c += 2) {
+                        v4i even_row, odd_row;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) {
+                            const int give = odd ? v[c][d] : v[c + 1][d];
+                            const int take = __builtin_amdgcn_update_dpp(0, give, 0xb1, 0xf, 0xf, true);    // lane ^ 1
+                            even_row[d] = odd ? take : v[c][d];
+                            odd_row[d] = odd ? v[c + 1][d] : take;
+                        }
+                        const bool in = at + odd * RUN + c * RUN < (uint32_t)p.N;
+                        if (in && row - odd < (uint32_t)p.M) *reinterpret_cast<v4i *>(dst + c * RUN) = even_row;
+                        if (in && row - odd + 1 < (uint32_t)p.M) *reinterpret_cast<v4i *>(dst + p.N + c * RUN) = odd_row;
+                    }
                 }
             }
             return;

@@ -131,20 +131,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p
     constexpr int APART = sizeof(windows[0]) / 16;
 #pragma unroll
     for (int f = 0; f < MT * NT; ++f) part[wave * APART + f * 64 + lane] = acc[f / NT][f % NT];
+    // a wave adds up and stores one fragment, or two side by side
     constexpr int MINE = (MT * NT + WAVES - 1) / WAVES;
-    Mx4Ends<1> ends[MINE];
-#pragma unroll
-    for (int k = 0; k < MINE; ++k) ends[k].load(p, n0 + (k * WAVES + wave) % NT * 16 + 4 * g);
+    static_assert(NT % MINE == 0 && MT * NT % MINE == 0, "");
+    const int f = wave * MINE;
+    const uint32_t o = n0 + f % NT * 16 + 4 * g;
+    Mx4Ends<MINE> ends;
+    ends.load(p, o);
     __syncthreads();
+    if (f >= MT * NT) return;
     const int used = (turns + share - 1) / share;
+    v4f v[1][MINE];
 #pragma unroll
     for (int k = 0; k < MINE; ++k) {
-        const int f = k * WAVES + wave;
-        if (f >= MT * NT) continue;
-        v4f v[1][1] = {{part[f * 64 + lane]}};
-        for (int s = 1; s < used; ++s) v[0][0] += part[s * APART + f * 64 + lane];
-        store_tile<1, 1>(p, v, ends[k], m0 + f / NT * 16 + r, n0 + f % NT * 16 + 4 * g);
+        v[0][k] = part[(f + k) * 64 + lane];
+        for (int s = 1; s < used; ++s) v[0][k] += part[s * APART + (f + k) * 64 + lane];
     }
+    store_tile<1, MINE>(p, v, ends, m0 + f / NT * 16 + r, o);
 }
 
 template <bool MASKED, int MT, int NT> static int launch_wave(const char *fn, Mx4Args p, hipStream_t s)

@@ -161,12 +161,14 @@ template <int MW, int NW, int MT, int NT> static int launch_held(const char *fn,
 
 int launch_mx4_tile_held(const char *fn, const Mx4Args &p, hipStream_t s)
 {
-    // large tiles where they keep three quarters of the compute units busy, small ones until every compute unit has
-    // its two blocks of the middle ones (256 x 256, 128 x 128, 64 x 128: 300 x 28672 x 8192 60.8, 61.6 and 87.5 us;
-    // 512 x 14336 x 4096 36.8, 26.3, 32.1; 512 x 4096 x 4096 33.6, 16.4, 11.8)
-    if ((long long)ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) return launch_held<2, 4, 8, 4>(fn, p, s);
-    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 128) > 256) return launch_held<2, 2, 4, 4>(fn, p, s);
-    return launch_held<1, 4, 4, 2>(fn, p, s);
+    // The smallest tile of which no compute unit gets a second one, from there on the largest (64 x 128, 128 x 128,
+    // 128 x 256 and 256 x 256: 512 x 4096 x 4096 10.3, 13.2, 19.2, 27.3 us; 1024 x 4096 x 4096 16.5, 14.3, 20.2, 28.2;
+    // 1024 x 8192 x 8192 55.9, 42.9, 40.4, 50.1; 768 x 14336 x 4096 42.3, 32.7, 39.3, 29.7)
+    auto tiles = [&](int rows, int outputs) { return (long long)ceil_div(p.M, rows) * ceil_div(p.N, outputs); };
+    if (tiles(64, 128) <= 256) return launch_held<1, 4, 4, 2>(fn, p, s);
+    if (tiles(128, 128) <= 256) return launch_held<2, 2, 4, 4>(fn, p, s);
+    if (tiles(128, 256) <= 256) return launch_held<2, 4, 4, 4>(fn, p, s);
+    return launch_held<2, 4, 8, 4>(fn, p, s);
 }
 
 }  // namespace mbu

@@ -125,10 +125,10 @@ template <int MT, int NT> static int launch_masked(const char *fn, Mx4Args p, hi
 
 int launch_mx4_tile_masked(const char *fn, const Mx4Args &p, hipStream_t s)
 {
-    // large tiles where every compute unit has its two blocks of them (128 x 256 against 64 x 128: 2048 x 8192 x 8192
-    // 64.8 and 77.0 us, 300 x 28672 x 8192 54.1 and 47.9, 1024 x 4096 x 4096 24.2 and 13.4)
-    if ((long long)ceil_div(p.M, 128) * ceil_div(p.N, 256) >= 512) return launch_masked<8, 4>(fn, p, s);
-    return launch_masked<4, 2>(fn, p, s);
+    // small tiles where every compute unit holds all of its share at once, two of them (64 x 128 against 128 x 256:
+    // 1024 x 4096 x 4096 12.0 and 18.2 us, 512 x 14336 x 4096 21.4 and 19.2, 2048 x 8192 x 8192 74.2 and 58.8)
+    if ((long long)ceil_div(p.M, 64) * ceil_div(p.N, 128) <= 512) return launch_masked<4, 2>(fn, p, s);
+    return launch_masked<8, 4>(fn, p, s);
 }
 
 }  // namespace mbu

@@ -147,8 +147,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
             fetch_rows(window + k * FEW_WINDOW, p.x, p.xs, 0, p.M, pitch, spitch, wave + k * waves, lane);
             load_weights(k, tile);
         }
-        __builtin_amdgcn_s_waitcnt(VM_0);                          // what was fetched into the windows is there
-        __builtin_amdgcn_sched_barrier(0);
+        wait_for<VM_0>();                                            // what was fetched into the windows is there
 #pragma unroll
         for (int k = 0; k < SW; ++k) {
             v4i s;
@@ -203,8 +202,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx4_few_kernel(const Mx4Args p
         };
         if constexpr (!MASKED)
             if (turn) {
-                __builtin_amdgcn_s_waitcnt(VM_0);                  // what was fetched into the windows is there
-                __builtin_amdgcn_sched_barrier(0);
+                wait_for<VM_0>();                                    // what was fetched into the windows is there
 #pragma unroll
                 for (int k = 0; k < SW; ++k) take_rows(w[k].c, w[k].s, window + k * FEW_WINDOW, r, g);
             }

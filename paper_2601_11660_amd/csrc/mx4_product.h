@@ -38,6 +38,13 @@ __device__ __forceinline__ void load4_to_lds(__amdgpu_buffer_rsrc_t rs, v4i *to,
                                              __builtin_amdgcn_readfirstlane(off), 0, 0);
 }
 constexpr int LGKM_0 = 0xc07f, VM_0 = 0x0f70;                       // s_waitcnt lgkmcnt(0), vmcnt(0)
+// ... and nothing that follows comes before it
+template <int COUNTS> __device__ __forceinline__ void wait_for()
+{
+    __builtin_amdgcn_s_waitcnt(COUNTS);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 __device__ __forceinline__ uint32_t load4(__amdgpu_buffer_rsrc_t rs, int lane_off, int off)
 {
     return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, lane_off, __builtin_amdgcn_readfirstlane(off), 0);

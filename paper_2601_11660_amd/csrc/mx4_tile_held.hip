@@ -111,8 +111,7 @@ __global__ __launch_bounds__(64 * MW * NW, MT * NT > 32 ? 1 : 2) void mx4_tile_h
                 constexpr int G = decltype(group)::value, i = G % MT, j = 2 * H + G / MT;
                 if constexpr (G == WHOLE) {
                     // LDS answers in order: the writes are done, only the reads of the groups since may be on their way
-                    __builtin_amdgcn_s_waitcnt(LGKM_0 | (WHOLE - SPAN) << 8);
-                    asm volatile("" ::: "memory");
+                    wait_for<LGKM_0 | (WHOLE - SPAN) << 8>();
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                     __builtin_amdgcn_sched_barrier(0);

@@ -75,8 +75,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p
     for (int turn = begin; turn < end; ++turn) {
         const int part = (turn - begin) & 3;
         // what was fetched into the window is there
-        __builtin_amdgcn_s_waitcnt(VM_0);
-        __builtin_amdgcn_sched_barrier(0);
+        wait_for<VM_0>();
         if (part == 0) {
 #pragma unroll
             for (int q = 0; q < SU; ++q) scales[q * 64 + lane] = ss[q];
@@ -111,8 +110,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p
         }
         // the next turn goes into the same window, as soon as this one's operands are out of it
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(LGKM_0);
-        __builtin_amdgcn_sched_barrier(0);
+        wait_for<LGKM_0>();
         fetch(turn + 1);
         if (part == 0) fetch_scales(turn + 4);
         __builtin_amdgcn_sched_barrier(0);
@@ -126,7 +124,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_wave_kernel(const Mx4Args p
             for (int n = 0; n < NT; ++n) acc[i][n] = mx4_mfma<1>(w[1][n], ws[n], x[1][i], xs[i], acc[i][n]);
     }
 
-    // every wave adds up some of the fragments
+    // every wave adds up some of the fragments; they take the place of the window, for which zeros may be on their way
+    wait_for<VM_0>();
     v4f *const part = reinterpret_cast<v4f *>(windows[0]);
     constexpr int APART = sizeof(windows[0]) / 16;
 #pragma unroll

@@ -5,7 +5,8 @@ namespace mbu {
 
 // Rows with consecutive values.  Eight values a thread, so four threads share a block's scale (two lane exchanges
 // inside a quad); `tpr` threads (a power of two) walk along a row, UNROLL groups of eight each with all loads in flight.
-// Rows are read 16 bytes at a time wherever they start; WHOLE: K is a multiple of eight.
+// Rows are read 16 bytes at a time wherever they start; WHOLE: K is a multiple of eight.  8192 x 8192 of bfloat16 and
+// back: 28 and 30 us, 170 MB each, 5.9 TB/s: the memory's rate.
 constexpr int QUANT_UNROLL = 4;
 
 template <int TYPE, bool WHOLE>
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restric
 // Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes blocks of its own rows, one of
 // float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four waves take eight
 // consecutive blocks of these rows and put the codes together in LDS, so that 128 consecutive bytes of a row are
-// written at a time; written by the lanes, 16 bytes here and there, 8192 x 8192 of bfloat16 took 76 us.
+// written at a time: 8192 x 8192 of bfloat16 46 us (written by the lanes, 16 bytes here and there, 76).
 constexpr int ACROSS_K = 256;
 template <int TYPE> struct AcrossRows {
     static constexpr int PER_LANE = TYPE == MBU_FLOAT32 ? 1 : 2;

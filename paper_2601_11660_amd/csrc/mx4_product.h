@@ -116,79 +116,90 @@ __device__ __forceinline__ v4i eight_in_a_row(v2i a, v2i b)
     return v;
 }
 
-template <int MT, int NT, typename OT>
-__device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
-                                         uint32_t o)
+// The values that fit into V, at outputs `at` and up of a row, wherever they start (the hardware takes any address);
+// nothing where the row ends among them.
+template <typename OT, typename V> __device__ __forceinline__ void store_whole(const Mx4Args &p, uint32_t row, uint32_t at, V v)
 {
-    constexpr int WIDE = 16 / (int)sizeof(OT), RUN = 4 * WIDE, RUNS = 16 * NT / RUN;
-    if constexpr (RUNS >= 1)
-        if (p.N % WIDE == 0) {
-            // Runs of 64 bytes of a row by four lanes, and where there are two of them 128 by eight, an even row and the
-            // odd one behind it in turn: the even row's lanes give their second run for the odd row's first.
-            const uint32_t first = __builtin_amdgcn_readfirstlane(o), at = first + (o - first) / 4 * WIDE, odd = m & 1;
+    if (row < (uint32_t)p.M && at + sizeof(V) / sizeof(OT) <= (uint32_t)p.N)
+        __builtin_memcpy((OT *)p.out + (uint64_t)row * (uint32_t)p.N + at, &v, sizeof(V));
+}
+
+template <int MT, int NT, typename OT>
+__device__ __forceinline__ void store_as(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+{
+    constexpr int RUN = 64 / (int)sizeof(OT), RUNS = 16 * NT / RUN, WIDE = RUNS ? 16 / (int)sizeof(OT) : 4;
+    const uint32_t first = __builtin_amdgcn_readfirstlane(o);
+    if constexpr (RUNS >= 1) {
+        // Runs of 64 bytes of a row by four lanes, and where there are two of them 128 by eight, an even row and the odd
+        // one behind it in turn: the even row's lanes give their second run for the odd row's first.  (8192 x 8192 x 1024,
+        // bfloat16: 57 us, 8191 outputs 65; stored as the products lie, 32 bytes at a time or value by value, 93 and 147.)
+        static_assert(RUNS == 1 || RUNS % 2 == 0, "");
+        const uint32_t at = first + (o - first) / 4 * WIDE, odd = m & 1;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                v4i v[RUNS];
+        for (int i = 0; i < MT; ++i) {
+            v4i v[RUNS];
 #pragma unroll
-                for (int c = 0; c < RUNS; ++c)
-                    if constexpr (sizeof(OT) == 2)
-                        v[c] = eight_in_a_row(mx4_pack4<OT>(ends.apply(2 * c, acc[i][2 * c])),
-                                              mx4_pack4<OT>(ends.apply(2 * c + 1, acc[i][2 * c + 1])));
-                    else
-                        v[c] = __builtin_bit_cast(v4i, ends.apply(c, acc[i][c]));
-                const uint32_t row = m + 16 * i;
-                if constexpr (RUNS == 1) {
-                    if (row < (uint32_t)p.M && at < (uint32_t)p.N)
-                        *reinterpret_cast<v4i *>((OT *)p.out + (uint64_t)row * (uint32_t)p.N + at) = v[0];
-                } else {
-                    static_assert(RUNS % 2 == 0, "");
-                    OT *const dst = (OT *)p.out + (uint64_t)(row - odd) * (uint32_t)p.N + at + odd * RUN;
+            for (int c = 0; c < RUNS; ++c)
+                if constexpr (sizeof(OT) == 2)
+                    v[c] = eight_in_a_row(mx4_pack4<OT>(acc[i][2 * c]), mx4_pack4<OT>(acc[i][2 * c + 1]));
+                else
+                    v[c] = __builtin_bit_cast(v4i, acc[i][c]);
+            if constexpr (RUNS == 1) store_whole<OT>(p, m + 16 * i, at, v[0]);
+            else
 #pragma unroll
-                    for (int c = 0; c < RUNS; c += 2) {
-                        v4i even_row, odd_row;
+                for (int c = 0; c < RUNS; c += 2) {
+                    v4i even_row, odd_row;
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) {
-                            const int give = odd ? v[c][d] : v[c + 1][d];
-                            const int take = __builtin_amdgcn_update_dpp(0, give, 0xb1, 0xf, 0xf, true);    // lane ^ 1
-                            even_row[d] = odd ? take : v[c][d];
-                            odd_row[d] = odd ? v[c + 1][d] : take;
-                        }
-                        const bool in = at + odd * RUN + c * RUN < (uint32_t)p.N;
-                        if (in && row - odd < (uint32_t)p.M) *reinterpret_cast<v4i *>(dst + c * RUN) = even_row;
-                        if (in && row - odd + 1 < (uint32_t)p.M) *reinterpret_cast<v4i *>(dst + p.N + c * RUN) = odd_row;
+                    for (int d = 0; d < 4; ++d) {
+                        const int give = odd ? v[c][d] : v[c + 1][d];
+                        const int take = __builtin_amdgcn_update_dpp(0, give, 0xb1, 0xf, 0xf, true);        // lane ^ 1
+                        even_row[d] = odd ? take : v[c][d];
+                        odd_row[d] = odd ? v[c + 1][d] : take;
                     }
+                    store_whole<OT>(p, m + 16 * i - odd, at + (c + odd) * RUN, even_row);
+                    store_whole<OT>(p, m + 16 * i - odd + 1, at + (c + odd) * RUN, odd_row);
                 }
-            }
-            return;
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                store_whole<OT>(p, m + 16 * i, o + 16 * n, mx4_pack4<OT>(acc[i][n]));
+    }
+    // the outputs that are left at the end of a row, one by one
+    const uint32_t left = (uint32_t)p.N / WIDE * WIDE;
+    if (left == (uint32_t)p.N || first + 16 * NT <= left) return;
 #pragma unroll
     for (int n = 0; n < NT; ++n, o += 16) {
-        if (o >= (uint32_t)p.N) continue;
-        const int left = (int)min(4u, (uint32_t)p.N - o);
+        if (o + 4 <= left || o >= (uint32_t)p.N) continue;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             if (m + 16 * i >= (uint32_t)p.M) continue;
-            const v4f v = ends.apply(n, acc[i][n]);
-            OT *dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + o;
-            if ((p.N & 3) == 0) mx4_store4(dst, v);
-            else
+            v4f v = acc[i][n];
+            asm volatile("" : "+v"(v));                           // rounded here: kept from above they need registers
+            OT *const dst = (OT *)p.out + (uint64_t)(m + 16 * i) * (uint32_t)p.N + o;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (q < left) mx4_store(dst + q, v[q]);
+            for (int q = 0; q < 4; ++q)
+                if (o + q >= left && o + q < (uint32_t)p.N) mx4_store(dst + q, v[q]);
         }
     }
 }
 // Factor, bias, the one rounding, and the stores of a wave: acc[i][n] holds outputs o + 16 n + 0..3 of row m + 16 i.
 template <int MT, int NT>
-__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
+__device__ __forceinline__ void store_tile(const Mx4Args &p, v4f (&acc)[MT][NT], const Mx4Ends<NT> &ends, uint32_t m,
                                            uint32_t o)
 {
-    if (p.dtype == MBU_FLOAT32) store_as<MT, NT, float>(p, acc, ends, m, o);
-    else if (p.dtype == MBU_FLOAT16) store_as<MT, NT, _Float16>(p, acc, ends, m, o);
-    else store_as<MT, NT, __bf16>(p, acc, ends, m, o);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = ends.apply(n, acc[i][n]);
+    if (p.dtype == MBU_FLOAT32) store_as<MT, NT, float>(p, acc, m, o);
+    else if (p.dtype == MBU_FLOAT16) store_as<MT, NT, _Float16>(p, acc, m, o);
+    else store_as<MT, NT, __bf16>(p, acc, m, o);
 }
 template <int MT, int NT>
-__device__ __forceinline__ void store_tile(const Mx4Args &p, const v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
+__device__ __forceinline__ void store_tile(const Mx4Args &p, v4f (&acc)[MT][NT], uint32_t m, uint32_t o)
 {
     Mx4Ends<NT> ends;
     ends.load(p, o);

@@ -8,7 +8,7 @@
 // nobody.  The sums are added up in LDS at the end, in the waves' order.  (Tiles of 64 x 64 whose four waves share
 // operands and barriers took 0.76 us for 512 inputs; 200 x 4096 x 14336 25.4 us, here 17.3.)
 //
-// 777 x 1001 x 2050 with float32 outputs 7.8 us, 64 x 4096 x 4096 5.0; masked 200 x 4096 x 14336 12.2.  Two windows a wave,
+// 777 x 1001 x 2050 with float32 outputs 7.1 us, 64 x 4096 x 4096 5.0; masked 200 x 4096 x 14336 12.2.  Two windows a wave,
 // fetched two turns ahead, were slower (12.0 for 10.7 us at 100 x 4095 x 11008): the address unit is the limit, not the wait.
 #include "mx4_product.h"
 

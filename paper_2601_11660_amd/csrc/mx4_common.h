@@ -200,7 +200,5 @@ template <typename T> __device__ __forceinline__ v2i mx4_pack4(v4f v)
     typedef T v4t __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(v2i, (v4t){(T)v.x, (T)v.y, (T)v.z, (T)v.w});
 }
-__device__ __forceinline__ void mx4_store4(float *p, v4f v) { *reinterpret_cast<v4f *>(p) = v; }
-template <typename T> __device__ __forceinline__ void mx4_store4(T *p, v4f v) { *reinterpret_cast<v2i *>(p) = mx4_pack4<T>(v); }
 
 }  // namespace mbu

@@ -6,7 +6,7 @@ namespace mbu {
 // Rows with consecutive values.  Eight values a thread, so four threads share a block's scale (two lane exchanges
 // inside a quad); `tpr` threads (a power of two) walk along a row, UNROLL groups of eight each with all loads in flight.
 // Rows are read 16 bytes at a time wherever they start; WHOLE: K is a multiple of eight.  8192 x 8192 of bfloat16 and
-// back: 28 and 30 us, 170 MB each, 5.9 TB/s: the memory's rate.
+// back: 28 us each way, 170 MB, 6 TB/s: the memory's rate and some help of the last-level cache.
 constexpr int QUANT_UNROLL = 4;
 
 template <int TYPE, bool WHOLE>
@@ -141,7 +141,8 @@ __device__ __forceinline__ void mx4_values(uint32_t q, uint32_t s, float v[8])
     }
 }
 
-// K a multiple of what 16 bytes of output hold: a thread writes 16 bytes.
+// A thread writes 16 bytes, wherever the row starts, and value by value where it ends among them.  (8192 x 8191 of bfloat16
+// 33 us; 16 aligned bytes at a time of the output as one array, pieced together across the rows' ends, 40.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__restrict__ codes,
                                                              const uint8_t *__restrict__ scales, int rows, int K, int kp,
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
     uint32_t q[QUANT_UNROLL], s[QUANT_UNROLL];
 #pragma unroll
     for (int u = 0; u < QUANT_UNROLL; ++u) {
-        const int k = min((first + u * tpr) * EACH, K - EACH);
+        const int k = min((first + u * tpr) * EACH, kp - EACH);
         const uint8_t *const at = codes + row * (kp >> 1) + (k >> 1);
         q[u] = EACH == 8 ? *reinterpret_cast<const uint32_t *>(at) : *reinterpret_cast<const uint16_t *>(at);
         s[u] = scales[row * (kp >> 5) + (k >> 5)];
@@ -169,73 +170,18 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *__re
         mx4_values(q[u], s[u], v);
         if (k >= K) break;
         T *const dst = (T *)out + row * K + k;
-        mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
-        if (EACH == 8) mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
-    }
-}
-
-// Any K: rows of the output start anywhere, so the output is taken as one array and a thread writes 16 aligned bytes of
-// it.  Its values are consecutive nibbles of one row, of at most two blocks, and of the next row's first block where the
-// row ends among them (K < 8: value by value).
-template <int TYPE>
-__global__ __launch_bounds__(256) void mx4_dequantize_ragged_kernel(const uint8_t *__restrict__ codes,
-                                                                    const uint8_t *__restrict__ scales, int K, int kp,
-                                                                    long long total, void *__restrict__ out)
-{
-    using T = typename Mx4Type<TYPE>::T;
-    constexpr int EACH = 16 / sizeof(T);
-    const long long first = (long long)blockIdx.x * (256 * EACH * QUANT_UNROLL);   // the block's first value
-    const long long row0 = total >> 32 ? first / K : (uint32_t)first / (uint32_t)K;
-    auto scale_of = [](uint32_t s) {                                          // 2^-127 is a subnormal, 255 a NaN
-        return __uint_as_float(s == 255u ? 0x7fc00000u : s == 0u ? 0x00400000u : s << 23);
-    };
-#pragma unroll
-    for (int u = 0; u < QUANT_UNROLL; ++u) {
-        const uint32_t k0 = (uint32_t)(first - row0 * K) + (u * 256 + threadIdx.x) * EACH;
-        const uint32_t down = k0 / (uint32_t)K;
-        const int k = (int)(k0 - down * (uint32_t)K);
-        const long long row = row0 + down, at = first + (u * 256 + threadIdx.x) * EACH;
-        if (at >= total) return;
-        T *const dst = (T *)out + at;
-        if (K >= EACH) {
-            const long long below = at + (K - k) < total ? row + 1 : row;       // the next row, if there is one
-            const uint8_t *const c = codes + row * (kp >> 1), *const sc = scales + row * (kp >> 5);
-            const int byte = min(k >> 1, (kp >> 1) - 8), here = min(EACH, K - k), last = min(k + EACH, K) - 1;
-            uint64_t w;
-            uint32_t next;
-            __builtin_memcpy(&w, c + byte, 8);
-            __builtin_memcpy(&next, codes + below * (kp >> 1), 4);
-            const float s0 = scale_of(sc[k >> 5]), s1 = scale_of(sc[last >> 5]), s2 = scale_of(scales[below * (kp >> 5)]);
-            uint32_t q = (uint32_t)(w >> (8 * ((k >> 1) - byte) + 4 * (k & 1)));
-            if (here < 8) q = (q & ((1u << 4 * here) - 1u)) | next << 4 * here;
-            const int same = 32 - (k & 31);                                   // values of the first block
-            const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
-                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
-            float v[8];
+        if (k + EACH <= K) {
+            v4i x;
+            if constexpr (EACH == 4) x = __builtin_bit_cast(v4i, (v4f){v[0], v[1], v[2], v[3]});
+            else {
+                const v2i lo = mx4_pack4<T>((v4f){v[0], v[1], v[2], v[3]}), hi = mx4_pack4<T>((v4f){v[4], v[5], v[6], v[7]});
+                x = (v4i){lo.x, lo.y, hi.x, hi.y};
+            }
+            __builtin_memcpy(dst, &x, 16);
+        } else
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                v[i] = (i & 1 ? p[i >> 1].y : p[i >> 1].x) * (i >= here ? s2 : i < same ? s0 : s1);
-            if (at + EACH <= total) {
-                mx4_store4(dst, (v4f){v[0], v[1], v[2], v[3]});
-                if (EACH == 8) mx4_store4(dst + 4, (v4f){v[4], v[5], v[6], v[7]});
-            } else {
-#pragma unroll
-                for (int i = 0; i < EACH; ++i)
-                    if (at + i < total) mx4_store(dst + i, v[i]);
-            }
-            continue;
-        }
-        long long r = row;
-        int c = k;
-        for (int i = 0; i < EACH && at + i < total; ++i) {
-            const uint32_t byte = codes[r * (kp >> 1) + (c >> 1)];
-            const v2f p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c & 1 ? byte >> 4 : byte, 1.0f, 0);
-            mx4_store(dst + i, p.x * scale_of(scales[r * (kp >> 5) + (c >> 5)]));
-            if (++c == K) {
-                c = 0;
-                ++r;
-            }
-        }
+                if (k + i < K) mx4_store(dst + i, v[i]);
     }
 }
 
@@ -283,10 +229,19 @@ __global__ __launch_bounds__(256) void mx4_pack_masked_kernel(const int8_t *__re
     dst[u] = make_uint4(sixteen_weights(x[0]), sixteen_weights(x[1]), sixteen_weights(x[2]), sixteen_weights(x[3]));
 }
 
+// Threads along a row (a power of two, 16 to 256) and pieces of a row.
 static int quant_geometry(int rows, int per_row, int *tpr_log, int *segs, long long *blocks)
 {
+    // one group of values a thread until the device is full, then all that it can have in flight (5000 x 1001 of float32:
+    // 6.3 and 5.4 us, back 5.9 and 5.0; 512 x 4096 of bfloat16 2.4 and 2.5)
+    const int each = (long long)rows * per_row >= 256 * 2048 ? QUANT_UNROLL : 1;
     int lg = 4;
-    while (lg < 8 && (1 << lg) < per_row) ++lg;
+    while (lg < 8 && (1 << lg) * each < per_row) ++lg;
+    // fewer threads for a row a little longer than they take at once, so that its last piece is not nearly empty (8191 x 8193
+    // of bfloat16 back: 47.8 and 34.4 us)
+    while (lg > 4 && ceil_div(per_row, (1 << lg) * QUANT_UNROLL) > 1 &&
+           ceil_div(per_row, (1 << lg) * QUANT_UNROLL) * (1 << lg) * QUANT_UNROLL > per_row + per_row / 8)
+        --lg;
     *tpr_log = lg;
     *segs = ceil_div(per_row, (1 << lg) * QUANT_UNROLL);
     *blocks = ((long long)rows + (256 >> lg) - 1) / (256 >> lg) * *segs;
@@ -331,17 +286,11 @@ static int dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int
 {
     constexpr int EACH = TYPE == MBU_FLOAT32 ? 4 : 8;
     const int kp = mx4_padded(K);
-    if (K % EACH == 0) {
-        int lg, segs;
-        long long blocks;
-        const int rc = quant_geometry(rows, K / EACH, &lg, &segs, &blocks);
-        if (rc) return rc;
-        MBU_LAUNCH((mx4_dequantize_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, rows, K, kp, lg, segs, out);
-    } else {
-        const long long total = (long long)rows * K, per = 256 * EACH * QUANT_UNROLL, blocks = (total + per - 1) / per;
-        if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_dequantize: tensor too large");
-        MBU_LAUNCH((mx4_dequantize_ragged_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, K, kp, total, out);
-    }
+    int lg, segs;
+    long long blocks;
+    const int rc = quant_geometry(rows, ceil_div(K, EACH), &lg, &segs, &blocks);
+    if (rc) return rc;
+    MBU_LAUNCH((mx4_dequantize_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, rows, K, kp, lg, segs, out);
     return check_launch("mbu_mx4_dequantize");
 }
 

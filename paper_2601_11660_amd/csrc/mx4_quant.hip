@@ -45,23 +45,24 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restric
 }
 
 // Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes blocks of its own rows, one of
-// float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four waves take eight
-// consecutive blocks of these rows and put the codes together in LDS, so that 128 consecutive bytes of a row are
-// written at a time: 8192 x 8192 of bfloat16 46 us (written by the lanes, 16 bytes here and there, 76).
+// float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four or eight waves take
+// eight consecutive blocks of these rows and put the codes together in LDS, so that 128 consecutive bytes of a row are
+// written at a time: 8192 x 8192 of bfloat16 41 us (written by the lanes, 16 bytes here and there, 76; with four waves 46),
+// of float32 66 (with eight waves 71).
 constexpr int ACROSS_K = 256;
 template <int TYPE> struct AcrossRows {
     static constexpr int PER_LANE = TYPE == MBU_FLOAT32 ? 1 : 2;
     static constexpr int ROWS = 64 * PER_LANE;
+    static constexpr int THREADS = 256 * PER_LANE;
 };
 
 template <int TYPE>
-__global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__restrict__ values, long long stride,
-                                                                  int rows, int K, int kp, int kgroups,
-                                                                  uint8_t *__restrict__ codes,
-                                                                  uint8_t *__restrict__ scales)
+__global__ __launch_bounds__(AcrossRows<TYPE>::THREADS) void mx4_quantize_across_kernel(
+    const void *__restrict__ values, long long stride, int rows, int K, int kp, int kgroups, uint8_t *__restrict__ codes,
+    uint8_t *__restrict__ scales)
 {
     using T = typename Mx4Type<TYPE>::T;
-    constexpr int PER_LANE = AcrossRows<TYPE>::PER_LANE, ROWS = AcrossRows<TYPE>::ROWS;
+    constexpr int PER_LANE = AcrossRows<TYPE>::PER_LANE, ROWS = AcrossRows<TYPE>::ROWS, THREADS = AcrossRows<TYPE>::THREADS;
     __shared__ uint4 code_tile[ROWS][9];                       // an odd number of units apart
     __shared__ uint8_t scale_tile[ROWS][8];
     const int tile = blockIdx.x / kgroups, kg = blockIdx.x - tile * kgroups;
@@ -73,8 +74,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__
     const bool odd = PER_LANE == 2 && row == from + 1;         // the last row alone: the upper half of what was read
     const bool single = PER_LANE == 2 && rows == 1;
 #pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-        const int block = turn * 4 + wave, k0 = kg * ACROSS_K + block * 32;
+    for (int turn = 0; turn < 512 / THREADS; ++turn) {
+        const int block = turn * (THREADS / 64) + wave, k0 = kg * ACROSS_K + block * 32;
         uint32_t v[32];
         if (!single) {
 #pragma unroll
@@ -113,19 +114,16 @@ __global__ __launch_bounds__(256) void mx4_quantize_across_kernel(const void *__
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < ROWS * 8 / 256; ++u) {
-        const int at = u * 256 + threadIdx.x, r = at >> 3, b = at & 7, k = kg * ACROSS_K + b * 32;
+    for (int u = 0; u < ROWS * 8 / THREADS; ++u) {
+        const int at = u * THREADS + threadIdx.x, r = at >> 3, b = at & 7, k = kg * ACROSS_K + b * 32;
         if (row0 + r < rows && k < kp)
             *reinterpret_cast<uint4 *>(codes + (row0 + r) * (kp >> 1) + (k >> 1)) = code_tile[r][b];
     }
     // four scales at a time: a row holds a multiple of four
-#pragma unroll
-    for (int u = 0; u < (ROWS * 2 + 255) / 256; ++u) {
-        const int at = u * 256 + threadIdx.x, r = at >> 1, b = (at & 1) * 4, k = kg * ACROSS_K + b * 32;
-        if (r < ROWS && row0 + r < rows && k < kp)
-            *reinterpret_cast<uint32_t *>(scales + (row0 + r) * (kp >> 5) + (k >> 5)) =
-                *reinterpret_cast<const uint32_t *>(&scale_tile[r][b]);
-    }
+    const int r = threadIdx.x >> 1, b = (threadIdx.x & 1) * 4, k = kg * ACROSS_K + b * 32;
+    if (r < ROWS && row0 + r < rows && k < kp)
+        *reinterpret_cast<uint32_t *>(scales + (row0 + r) * (kp >> 5) + (k >> 5)) =
+            *reinterpret_cast<const uint32_t *>(&scale_tile[r][b]);
 }
 
 // number of codes [8 i, 8 i + 8) -> values; every product of a code and a scale is exact in float32
@@ -257,8 +255,8 @@ static int quantize(const void *x, int rows, int K, long long stride, bool acros
         const int kg = ceil_div(kp, ACROSS_K);
         const long long blocks = ((long long)rows + AcrossRows<TYPE>::ROWS - 1) / AcrossRows<TYPE>::ROWS * kg;
         if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_quantize: tensor too large");
-        MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(256), 0, s, x, stride, rows, K, kp, kg,
-                   codes, scales);
+        MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(AcrossRows<TYPE>::THREADS), 0, s, x, stride,
+                   rows, K, kp, kg, codes, scales);
         return check_launch("mbu_mx4_quantize");
     }
     int lg, segs;

@@ -11,10 +11,10 @@
 // window whole, so that the first operands of phase t + 1 are read before phase t ends and no wave waits for them.  The
 // barrier at the start of a phase stands before the writes: by then every wave has multiplied what it read there.
 //
-// 8192 x 8192 x 8192, bfloat16 out: 250 us, 4.4 PFLOP/s of the 7.1 that this instruction reaches on registers full of random
-// codes, at a clock of 1.8 GHz; the matrix pipes are busy for 59 % of the cycles, LDS for 46 %.  What it costs to bring
+// 8192 x 8192 x 8192, bfloat16 out: 250-257 us, 4.3-4.4 PFLOP/s of the 7.1 that this instruction reaches on registers full
+// of random codes, at a clock of 1.8 GHz; the matrix pipes are busy for 59 % of the cycles, LDS for 46 %.  What it costs to bring
 // the operands into LDS is what is left: without the fetches and the writes the loop took 170 us, without the writes
-// 200, without the fetches 219; without the barriers, without reading the weights from LDS, with all fetches from the
+// 214, without the fetches 219; without the barriers, without reading the weights from LDS, with all fetches from the
 // second-level cache it gained 4, 1 and 2 %.  Loads that go to LDS by themselves gained nothing: with 128 bytes of a row at
 // a time there is room for one phase on its way (270 us), with 64 bytes for three (272).
 #include "mx4_product.h"

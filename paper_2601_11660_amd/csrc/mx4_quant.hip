@@ -44,27 +44,26 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restric
     }
 }
 
-// Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes blocks of its own rows, one of
-// float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four or eight waves take
-// eight consecutive blocks of these rows and put the codes together in LDS, so that 128 consecutive bytes of a row are
-// written at a time: 8192 x 8192 of bfloat16 41 us (written by the lanes, 16 bytes here and there, 76; with four waves 46),
-// of float32 66 (with eight waves 71).
-constexpr int ACROSS_K = 256;
+// Rows whose values lie `stride` apart, neighbouring rows next to each other: a lane takes a block of its own rows, one of
+// float32 or two of the 16-bit types (four bytes a load), 64 consecutive lanes per wave.  A block's four waves take four
+// consecutive blocks of these rows and put the codes together in LDS, so that 64 consecutive bytes of a row are written
+// at a time: 8192 x 8192 of bfloat16 40 us, of float32 64, 5000 x 1001 of float32 5.5 (written by the lanes, 16 bytes here
+// and there, 8192 x 8192 of bfloat16 took 76; with eight blocks, two a wave, 46, 66 and 6.6).
+constexpr int ACROSS_BLOCKS = 4;
 template <int TYPE> struct AcrossRows {
     static constexpr int PER_LANE = TYPE == MBU_FLOAT32 ? 1 : 2;
     static constexpr int ROWS = 64 * PER_LANE;
-    static constexpr int THREADS = 256 * PER_LANE;
 };
 
 template <int TYPE>
-__global__ __launch_bounds__(AcrossRows<TYPE>::THREADS) void mx4_quantize_across_kernel(
+__global__ __launch_bounds__(64 * ACROSS_BLOCKS) void mx4_quantize_across_kernel(
     const void *__restrict__ values, long long stride, int rows, int K, int kp, int kgroups, uint8_t *__restrict__ codes,
     uint8_t *__restrict__ scales)
 {
     using T = typename Mx4Type<TYPE>::T;
-    constexpr int PER_LANE = AcrossRows<TYPE>::PER_LANE, ROWS = AcrossRows<TYPE>::ROWS, THREADS = AcrossRows<TYPE>::THREADS;
-    __shared__ uint4 code_tile[ROWS][9];                       // an odd number of units apart
-    __shared__ uint8_t scale_tile[ROWS][8];
+    constexpr int PER_LANE = AcrossRows<TYPE>::PER_LANE, ROWS = AcrossRows<TYPE>::ROWS;
+    __shared__ uint4 code_tile[ROWS][ACROSS_BLOCKS + 1];       // an odd number of units apart
+    __shared__ __align__(4) uint8_t scale_tile[ROWS][ACROSS_BLOCKS];
     const int tile = blockIdx.x / kgroups, kg = blockIdx.x - tile * kgroups;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long row0 = (long long)tile * ROWS, row = row0 + lane * PER_LANE;
@@ -73,57 +72,53 @@ __global__ __launch_bounds__(AcrossRows<TYPE>::THREADS) void mx4_quantize_across
     const T *const x = (const T *)values + from;
     const bool odd = PER_LANE == 2 && row == from + 1;         // the last row alone: the upper half of what was read
     const bool single = PER_LANE == 2 && rows == 1;
+    const int k0 = (kg * ACROSS_BLOCKS + wave) * 32;
+    uint32_t v[32];
+    if (!single) {
 #pragma unroll
-    for (int turn = 0; turn < 512 / THREADS; ++turn) {
-        const int block = turn * (THREADS / 64) + wave, k0 = kg * ACROSS_K + block * 32;
-        uint32_t v[32];
-        if (!single) {
+        for (int i = 0; i < 32; ++i) __builtin_memcpy(&v[i], x + min(k0 + i, K - 1) * stride, 4);
+    } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) __builtin_memcpy(&v[i], x + min(k0 + i, K - 1) * stride, 4);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                uint16_t one;
-                __builtin_memcpy(&one, x + min(k0 + i, K - 1) * stride, 2);
-                v[i] = one;
-            }
+        for (int i = 0; i < 32; ++i) {
+            uint16_t one;
+            __builtin_memcpy(&one, x + min(k0 + i, K - 1) * stride, 2);
+            v[i] = one;
         }
+    }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = k0 + i < K ? odd ? v[i] >> 16 : v[i] : 0u;
+    for (int i = 0; i < 32; ++i) v[i] = k0 + i < K ? odd ? v[i] >> 16 : v[i] : 0u;
 #pragma unroll
-        for (int e = 0; e < PER_LANE; ++e) {
-            Mx4In<T> in[4];
+    for (int e = 0; e < PER_LANE; ++e) {
+        Mx4In<T> in[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < 8 / PER_LANE; ++i)       // two 16-bit values of one row side by side
-                    in[j].v[i] = PER_LANE == 1 ? v[8 * j + i]
-                                               : __builtin_amdgcn_perm(v[8 * j + 2 * i + 1], v[8 * j + 2 * i],
-                                                                       e ? 0x07060302u : 0x05040100u);
-            uint32_t top = 0;
+            for (int i = 0; i < 8 / PER_LANE; ++i)       // two 16-bit values of one row side by side
+                in[j].v[i] = PER_LANE == 1 ? v[8 * j + i]
+                                           : __builtin_amdgcn_perm(v[8 * j + 2 * i + 1], v[8 * j + 2 * i],
+                                                                   e ? 0x07060302u : 0x05040100u);
+        uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = max(top, in[j].top());
-            const uint32_t s = mx4_scale_byte(top);
-            const float scale = mx4_scale_float(s);
-            uint32_t q[4];
+        for (int j = 0; j < 4; ++j) top = max(top, in[j].top());
+        const uint32_t s = mx4_scale_byte(top);
+        const float scale = mx4_scale_float(s);
+        uint32_t q[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = s == 255u ? 0u : in[j].codes(scale);
-            code_tile[lane * PER_LANE + e][block] = make_uint4(q[0], q[1], q[2], q[3]);
-            scale_tile[lane * PER_LANE + e][block] = (uint8_t)s;
-        }
+        for (int j = 0; j < 4; ++j) q[j] = s == 255u ? 0u : in[j].codes(scale);
+        code_tile[lane * PER_LANE + e][wave] = make_uint4(q[0], q[1], q[2], q[3]);
+        scale_tile[lane * PER_LANE + e][wave] = (uint8_t)s;
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < ROWS * 8 / THREADS; ++u) {
-        const int at = u * THREADS + threadIdx.x, r = at >> 3, b = at & 7, k = kg * ACROSS_K + b * 32;
-        if (row0 + r < rows && k < kp)
-            *reinterpret_cast<uint4 *>(codes + (row0 + r) * (kp >> 1) + (k >> 1)) = code_tile[r][b];
+    for (int u = 0; u < ROWS / 64; ++u) {
+        const int at = u * (64 * ACROSS_BLOCKS) + threadIdx.x, r = at / ACROSS_BLOCKS, b = at % ACROSS_BLOCKS;
+        if (row0 + r < rows)                                       // Kp is a multiple of the blocks' 128 values
+            *reinterpret_cast<uint4 *>(codes + (row0 + r) * (kp >> 1) + (kg * ACROSS_BLOCKS + b) * 16) = code_tile[r][b];
     }
     // four scales at a time: a row holds a multiple of four
-    const int r = threadIdx.x >> 1, b = (threadIdx.x & 1) * 4, k = kg * ACROSS_K + b * 32;
-    if (r < ROWS && row0 + r < rows && k < kp)
-        *reinterpret_cast<uint32_t *>(scales + (row0 + r) * (kp >> 5) + (k >> 5)) =
-            *reinterpret_cast<const uint32_t *>(&scale_tile[r][b]);
+    if ((int)threadIdx.x < ROWS && row0 + threadIdx.x < rows)
+        *reinterpret_cast<uint32_t *>(scales + (row0 + threadIdx.x) * (kp >> 5) + kg * ACROSS_BLOCKS) =
+            *reinterpret_cast<const uint32_t *>(scale_tile[threadIdx.x]);
 }
 
 // number of codes [8 i, 8 i + 8) -> values; every product of a code and a scale is exact in float32
@@ -252,10 +247,10 @@ static int quantize(const void *x, int rows, int K, long long stride, bool acros
 {
     const int kp = mx4_padded(K);
     if (across) {
-        const int kg = ceil_div(kp, ACROSS_K);
+        const int kg = kp / (32 * ACROSS_BLOCKS);
         const long long blocks = ((long long)rows + AcrossRows<TYPE>::ROWS - 1) / AcrossRows<TYPE>::ROWS * kg;
         if (blocks > 0x7fffffffLL) return fail(MBU_ERR_SHAPE, "mbu_mx4_quantize: tensor too large");
-        MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(AcrossRows<TYPE>::THREADS), 0, s, x, stride,
+        MBU_LAUNCH((mx4_quantize_across_kernel<TYPE>), dim3((unsigned)blocks), dim3(64 * ACROSS_BLOCKS), 0, s, x, stride,
                    rows, K, kp, kg, codes, scales);
         return check_launch("mbu_mx4_quantize");
     }

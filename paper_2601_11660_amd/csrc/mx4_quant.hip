@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void *__restric
     const int tpr = 1 << tpr_log;
     const int group = blockIdx.x / segs, seg = blockIdx.x - group * segs;
     const long long row = (long long)group * (256 >> tpr_log) + (threadIdx.x >> tpr_log);
-    if (row >= rows) return;                       // whole quads: tpr is a multiple of 16
+    if (row >= rows) return;                       // whole quads: tpr is a multiple of 4
     const int first = seg * tpr * QUANT_UNROLL + (threadIdx.x & (tpr - 1));
     using T = typename Mx4Type<TYPE>::T;
     const T *src = (const T *)values + row * stride;
@@ -222,17 +222,17 @@ __global__ __launch_bounds__(256) void mx4_pack_masked_kernel(const int8_t *__re
     dst[u] = make_uint4(sixteen_weights(x[0]), sixteen_weights(x[1]), sixteen_weights(x[2]), sixteen_weights(x[3]));
 }
 
-// Threads along a row (a power of two, 16 to 256) and pieces of a row.
+// Threads along a row (a power of two, 4 to 256) and pieces of a row.
 static int quant_geometry(int rows, int per_row, int *tpr_log, int *segs, long long *blocks)
 {
     // one group of values a thread until the device is full, then all that it can have in flight (5000 x 1001 of float32:
-    // 6.3 and 5.4 us, back 5.9 and 5.0; 512 x 4096 of bfloat16 2.4 and 2.5)
+    // 6.3 and 5.4 us, back 5.9 and 5.0; 100000 x 100 of bfloat16 11.5 and 7.9; 512 x 4096 of bfloat16 2.4 and 2.5)
     const int each = (long long)rows * per_row >= 256 * 2048 ? QUANT_UNROLL : 1;
-    int lg = 4;
+    int lg = each > 1 ? 2 : 4;
     while (lg < 8 && (1 << lg) * each < per_row) ++lg;
     // fewer threads for a row a little longer than they take at once, so that its last piece is not nearly empty (8191 x 8193
     // of bfloat16 back: 47.8 and 34.4 us)
-    while (lg > 4 && ceil_div(per_row, (1 << lg) * QUANT_UNROLL) > 1 &&
+    while (lg > 2 && ceil_div(per_row, (1 << lg) * QUANT_UNROLL) > 1 &&
            ceil_div(per_row, (1 << lg) * QUANT_UNROLL) * (1 << lg) * QUANT_UNROLL > per_row + per_row / 8)
         --lg;
     *tpr_log = lg;

@@ -128,6 +128,25 @@ def test_nothing_else_is_read_or_written(m, n, k):
         assert bool((out[:64] == 5.5).all()) and bool((out[-64:] == 5.5).all())
 
 
+@pytest.mark.parametrize("rows, k", [(70000, 1), (40000, 100), (70000, 33), (5000, 1001), (530, 8193), (3, 8200), (16400, 257)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_conversions_of_many_rows(dtype, rows, k):
+    """Narrow and wide rows, from four threads a row to several pieces of one; along, across and back."""
+    say(f"mx4 conversions {rows}x{k} {dtype}")
+    x = torch.randn((rows, k), device="cuda").to(dtype)
+    codes, scales = B.mx4_quantize(x)
+    at = np.unique(np.random.default_rng(rows).integers(0, rows, 200).tolist() + [0, rows - 1])
+    pick = torch.from_numpy(at).cuda()
+    want, want_scales = R.quantize(x[pick].float().cpu().numpy())
+    assert np.array_equal(codes[pick].cpu().numpy(), want) and np.array_equal(scales[pick].cpu().numpy(), want_scales)
+    c2, s2 = B.mx4_quantize(x.t().contiguous().t())
+    assert torch.equal(c2, codes) and torch.equal(s2, scales)
+    back = B.mx4_dequantize(codes, scales, k, dtype)
+    assert torch.equal(back[pick].cpu(), torch.from_numpy(R.values(want, want_scales, k)).to(dtype))
+    # quantising what came back changes no value
+    assert torch.equal(B.mx4_dequantize(*B.mx4_quantize(back), k, dtype), back)
+
+
 def test_sign_of_zero_and_infinity_without_factor_and_bias():
     """Zeros stay zeros, and what is beyond the output's type is infinite."""
     say("mx4 signs of zero")

@@ -31,13 +31,11 @@ static bool overlap(const void *a, size_t na, const void *b, size_t nb)
 }
 
 // float rows: only the alignment of their type is needed
-static int check_float_rows(const char *fn, const void *x, int dtype, int rows, int K, long long stride)
+static int check_float_rows(const char *fn, const void *x, int dtype, long long stride)
 {
     if (!x) return fail(MBU_ERR_NULL, "%s: x is NULL", fn);
     if ((uintptr_t)x % float_size(dtype)) return fail(MBU_ERR_ALIGN, "%s: x is not aligned to its type", fn);
     if (stride < 0 || stride > (1ll << 40)) return fail(MBU_ERR_SHAPE, "%s: stride %lld out of range", fn, stride);
-    (void)rows;
-    (void)K;
     return MBU_OK;
 }
 // bytes from the first to behind the last value
@@ -122,7 +120,7 @@ static int linear(const char *fn, const void *x, int x_dtype, int M, long long s
     begin_call();
     int rc = check_dtype(fn, "x_dtype", x_dtype);
     if (!rc) rc = check_product(fn, M, p);
-    if (!rc) rc = check_float_rows(fn, x, x_dtype, M, p.K, stride);
+    if (!rc) rc = check_float_rows(fn, x, x_dtype, stride);
     if (rc) return rc;
     const size_t need = linear_workspace(M, p.K), n = (size_t)M * p.N * float_size(p.dtype);
     if (need) MBU_REQ_PTR(fn, workspace);
@@ -155,7 +153,7 @@ int mbu_mx4_quantize(const void *x, int x_dtype, int rows, int K, long long stri
     begin_call();
     int rc = check_rows(fn, "rows", rows, K);
     if (!rc) rc = check_dtype(fn, "x_dtype", x_dtype);
-    if (!rc) rc = check_float_rows(fn, x, x_dtype, rows, K, stride);
+    if (!rc) rc = check_float_rows(fn, x, x_dtype, stride);
     if (rc) return rc;
     if (across != 0 && across != 1) return fail(MBU_ERR_ARG, "%s: across must be 0 or 1, got %d", fn, across);
     MBU_REQ_PTR(fn, codes);

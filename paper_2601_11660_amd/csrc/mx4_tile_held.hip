@@ -11,7 +11,7 @@
 // window whole, so that the first operands of phase t + 1 are read before phase t ends and no wave waits for them.  The
 // barrier at the start of a phase stands before the writes: by then every wave has multiplied what it read there.
 //
-// 8192 x 8192 x 8192, bfloat16 out: 250-257 us, 4.3-4.4 PFLOP/s of the 7.1 that this instruction reaches on registers full
+// 8192 x 8192 x 8192, bfloat16 out: 250-260 us, 4.2-4.4 PFLOP/s of the 7.1 that this instruction reaches on registers full
 // of random codes, at a clock of 1.8 GHz; the matrix pipes are busy for 59 % of the cycles, LDS for 46 %.  What it costs to bring
 // the operands into LDS is what is left: without the fetches and the writes the loop took 170 us, without the writes
 // 214, without the fetches 219; without the barriers, without reading the weights from LDS, with all fetches from the
